@@ -309,6 +309,51 @@ xrl_status xrl_gae(int32_t device, int32_t num_steps, int32_t num_trajectories, 
                    const float* values, const uint8_t* done, float gamma, float lambda, float* adv, float* ret,
                    void* stream);
 
+/* ---- (5) policies over rows of logits: scoring, its gradient, the update -------------------------- */
+
+/* (The heads above score this library's own candidates.  These calls are for any other policy of a training or serving
+ * program, from a few masked actions to a vocabulary of tokens, whose logits the caller's own model has computed.)
+ *
+ * Each row of logits is a categorical distribution over the entries of its support: those its mask leaves, without the
+ * entries at -infinity, which count as masked.  With m the largest logit of the support and s the scale (1 / temperature),
+ *   l = ln sum_j exp(s (x_j - m)),   ln p_j = s (x_j - m) - l,   H = -sum_j p_j ln p_j.
+ *   dtype       XRL_FP32 or XRL_BF16, of the logits; sums and results are fp32
+ *   logits      DEVICE [rows x vocab], row r at logits + r * row_stride elements (row_stride >= vocab; any alignment
+ *               of a row that its elements have)
+ *   token       DEVICE int32 [rows], or NULL with logp NULL: the choice whose log probability is wanted; -1 = none in this row
+ *   mask        DEVICE u8 [rows x vocab] or NULL: 0 = entry is invalid and its logit, whatever it is, not looked at; rows
+ *               mask_stride bytes apart, 0 = one mask for all rows
+ *   scale       in (0, 1e6]
+ *   logp        DEVICE fp32 [rows] or NULL: ln p of the token; 0 for token -1, -infinity outside the support, NaN for a
+ *               token below -1 or at vocab and above
+ *   entropy     DEVICE fp32 [rows] or NULL: H; 0 for a row without support
+ *   norm        DEVICE fp32 [rows x 2] or NULL, 8-byte aligned: {m, l}, what xrl_logprob_grad needs; {-infinity, -infinity}
+ *               for a row without support.  (The log of the row's partition sum is s m + l.)
+ *   top_token   DEVICE int32 [rows x num_top], top_logp DEVICE fp32 [rows x num_top]: the num_top (0 to XRL_MAX_TOP, at most
+ *               vocab) largest logits of the support in falling order, equal ones by rising index, and their ln p; -1 and
+ *               -infinity where the support has fewer
+ * A row with a NaN or +infinity in its support gives NaN in logp, entropy, l and top_logp; its alternatives are the best of
+ * its other entries.  Sums are added in an order that depends on the sizes alone.  Needs no context; one launch; captures
+ * into a CUDA graph; nothing is allocated.  Errors: INVALID_ARG, UNSUPPORTED (num_top), CUDA. */
+#define XRL_MAX_TOP 32
+xrl_status xrl_logprob(int32_t device, int32_t dtype, int32_t rows, int32_t vocab, const void* logits, int64_t row_stride,
+                       const int32_t* token, const uint8_t* mask, int64_t mask_stride, float scale, int32_t num_top,
+                       float* logp, float* entropy, float* norm, int32_t* top_token, float* top_logp, void* stream);
+
+/* Gradient of logp and entropy with respect to the logits, for the gradients dlogp and dentropy of some objective:
+ *   grad_j = s [ dlogp (1[j = token] - p_j) - dentropy p_j (ln p_j + H) ]  in the support, exactly 0 outside.
+ *   logits, token, mask, scale    as given to xrl_logprob;   norm, entropy   what it returned
+ *   dlogp       DEVICE fp32 [rows] or NULL = 0 (token may then be NULL); not used in rows of token -1; a token out of range
+ *               makes its row NaN
+ *   dentropy    DEVICE fp32 [rows] or NULL = 0 (entropy may then be NULL)
+ *   grad        DEVICE [rows x vocab] of dtype, rows grad_stride elements apart, rounded once; may be `logits` itself (same
+ *               stride), otherwise the two must not overlap
+ * The alternatives have no gradient.  Needs no context; one launch.  Errors: INVALID_ARG, CUDA. */
+xrl_status xrl_logprob_grad(int32_t device, int32_t dtype, int32_t rows, int32_t vocab, const void* logits,
+                            int64_t row_stride, const int32_t* token, const uint8_t* mask, int64_t mask_stride, float scale,
+                            const float* norm, const float* dlogp, const float* entropy, const float* dentropy, void* grad,
+                            int64_t grad_stride, void* stream);
+
 /* Data-parallel training step (Section 3.3.4: the objective is a mean over the environments of the mini-batch;
  * the paper leaves training on several devices as future work).  Every rank has run xrl_ppo_grad on its own
  * environments, so its gradient and loss terms are means over n_r local environments.  The mean over all

@@ -26,7 +26,7 @@ EXPORTED_SYMBOLS = [
     "xrl_policy_value", "xrl_sample", "xrl_last_device_status", "xrl_launch_counts", "xrl_version",
     "xrl_profile", "xrl_profile_read", "xrl_pack_csr_static", "xrl_encode_delta", "xrl_delta_rows", "xrl_get_weights",
     "xrl_graph_begin", "xrl_graph_launch", "xrl_batch_set_edge_attr", "xrl_ppo_grad", "xrl_gae",
-    "xrl_grad_weigh", "xrl_grad_unweigh", "xrl_init_weights", "xrl_round_features",
+    "xrl_grad_weigh", "xrl_grad_unweigh", "xrl_init_weights", "xrl_round_features", "xrl_logprob", "xrl_logprob_grad",
 ]
 PROFILE_FAMILIES = ["pack", "node_update", "transform", "aggregate", "readout", "heads", "aggregate_readout",
                     "layers_fused"]
@@ -95,6 +95,8 @@ def load_library():
         "xrl_ppo_grad": [vp] * 8 + [C.c_float] * 3 + [vp] * 4,
         "xrl_gae": [i32, i32, i32, vp, vp, vp, C.c_float, C.c_float, vp, vp, vp],
         "xrl_graph_launch": [vp, vp],
+        "xrl_logprob": [i32, i32, i32, i32, vp, i64, vp, vp, i64, C.c_float, i32] + [vp] * 6,
+        "xrl_logprob_grad": [i32, i32, i32, i32, vp, i64, vp, vp, i64, C.c_float] + [vp] * 5 + [i64, vp],
         "xrl_grad_weigh": [i32, i32, i32, vp, i64, vp, i64, vp, vp],
         "xrl_grad_unweigh": [i32, i32, i32, vp, i64, vp, vp, C.POINTER(i64), vp],
     }
@@ -329,6 +331,114 @@ def xrl_gae(reward, values, done, gamma, lam, adv=None, ret=None, stream=None):
                                 C.c_float(gamma), C.c_float(lam), _dev_ptr(adv), _dev_ptr(ret), _stream(stream))
     _check(st, "xrl_gae")
     return adv, ret
+
+
+def _device_of(where, *tensors):
+    """The one CUDA device that all tensors (None: not given) are on."""
+    dev = next(t for t in tensors if t is not None).device
+    if dev.type != "cuda" or any(t is not None and t.device != dev for t in tensors):
+        raise XrlError(1, f"{where} (every tensor on one CUDA device)")
+    return dev.index
+
+
+def _storage(where, t):
+    name = str(t.dtype)
+    if name not in ("torch.float32", "torch.bfloat16"):
+        raise XrlError(8, f"{where} ({name}: float32 or bfloat16)")
+    return XRL_BF16 if name == "torch.bfloat16" else XRL_FP32
+
+
+def _stream_on(device, stream):
+    if stream is not None:
+        return C.c_void_p(int(stream))
+    import torch
+    return C.c_void_p(torch._C._cuda_getCurrentRawStream(device))
+
+
+def _flat(where, what, t, dtype, *shape):
+    """The pointer of an argument that has to be a contiguous tensor of this type and shape (or None)."""
+    if t is None:
+        return None
+    if str(t.dtype) != "torch." + dtype or tuple(t.shape) != shape or not t.is_contiguous():
+        raise XrlError(1, f"{where} ({what}: contiguous {dtype} {list(shape)})")
+    return t.data_ptr()
+
+
+def _rows_of(where, what, t, rows, vocab):
+    """(pointer, row stride) of a [rows x vocab] tensor whose rows may lie apart."""
+    if t.dim() != 2 or tuple(t.shape) != (rows, vocab) or (vocab > 1 and t.stride(1) != 1):
+        raise XrlError(1, f"{where} ({what}: [{rows} x {vocab}], entries of a row side by side)")
+    return t.data_ptr(), t.stride(0) if rows > 1 else vocab
+
+
+def _mask_of(where, mask, rows, vocab):
+    """(pointer, row stride) of a mask: uint8 or bool, [rows x vocab] or one row for all."""
+    if mask is None:
+        return None, 0
+    if str(mask.dtype) not in ("torch.uint8", "torch.bool") or mask.dim() not in (1, 2):
+        raise XrlError(1, f"{where} (mask: uint8 or bool, [rows x vocab], [1 x vocab] or [vocab])")
+    one = mask.dim() == 1 or (mask.shape[0] == 1 and rows != 1)
+    ptr, stride = _rows_of(where, "mask", mask if mask.dim() == 2 else mask[None], 1 if one else rows, vocab)
+    return ptr, 0 if one else stride
+
+
+def xrl_logprob(logits, token=None, mask=None, scale=1.0, top=0, out=None, stream=None):
+    """Rows of logits as categorical distributions (see include/xrl.h).  logits: torch CUDA [rows, vocab], float32 or
+    bfloat16, entries of a row side by side; token: int32 [rows], -1 = none; mask: uint8 or bool [rows, vocab], or one row
+    for all; top: how many alternatives.  Returns a dict: entropy [rows], norm [rows, 2], with a token logp [rows], with
+    alternatives top_token and top_logp [rows, top]; out: a dict an earlier call of the same sizes returned, to be
+    written again."""
+    where = "xrl_logprob"
+    import torch
+    if logits.dim() != 2:
+        raise XrlError(1, f"{where} (logits: [rows x vocab])")
+    rows, vocab = logits.shape
+    o = {} if out is None else out
+    dev = _device_of(where, logits, token, mask, *o.values())
+    if out is None:
+        new = lambda *shape, dtype=torch.float32: torch.empty(shape, dtype=dtype, device=logits.device)  # noqa: E731
+        o = {"entropy": new(rows), "norm": new(rows, 2)}
+        if token is not None:
+            o["logp"] = new(rows)
+        if top > 0:
+            o["top_token"], o["top_logp"] = new(rows, top, dtype=torch.int32), new(rows, top)
+    x, stride = _rows_of(where, "logits", logits, rows, vocab)
+    mp, mstride = _mask_of(where, mask, rows, vocab)
+    ptr = lambda name, dtype, *shape: _flat(where, name, o.get(name), dtype, *shape)  # noqa: E731
+    st = load_library().xrl_logprob(
+        dev, _storage(where, logits), rows, vocab, x, stride, _flat(where, "token", token, "int32", rows), mp, mstride, scale,
+        top, ptr("logp", "float32", rows), ptr("entropy", "float32", rows), ptr("norm", "float32", rows, 2),
+        ptr("top_token", "int32", rows, top), ptr("top_logp", "float32", rows, top), _stream_on(dev, stream))
+    _check(st, where)
+    return o
+
+
+def xrl_logprob_grad(logits, norm, token=None, dlogp=None, entropy=None, dentropy=None, mask=None, scale=1.0, grad=None,
+                     stream=None):
+    """The gradient of sum(dlogp * logp + dentropy * entropy) with respect to the logits: logits, token, mask, scale as given
+    to xrl_logprob, norm and entropy as it returned them; dlogp, dentropy: float32 [rows] or None = 0.  grad: like the logits
+    and of their type, may be the logits themselves; allocated (contiguous) if None."""
+    where = "xrl_logprob_grad"
+    import torch
+    if logits.dim() != 2:
+        raise XrlError(1, f"{where} (logits: [rows x vocab])")
+    rows, vocab = logits.shape
+    dev = _device_of(where, logits, norm, token, dlogp, entropy, dentropy, mask, grad)
+    if grad is None:
+        grad = torch.empty((rows, vocab), dtype=logits.dtype, device=logits.device)
+    dtype = _storage(where, logits)
+    if grad.dtype != logits.dtype:
+        raise XrlError(1, f"{where} (grad: the type of the logits)")
+    x, stride = _rows_of(where, "logits", logits, rows, vocab)
+    gp, gstride = _rows_of(where, "grad", grad, rows, vocab)
+    mp, mstride = _mask_of(where, mask, rows, vocab)
+    vec = lambda name, t: _flat(where, name, t, "float32", rows)  # noqa: E731
+    st = load_library().xrl_logprob_grad(
+        dev, dtype, rows, vocab, x, stride, _flat(where, "token", token, "int32", rows), mp, mstride, scale,
+        _flat(where, "norm", norm, "float32", rows, 2), vec("dlogp", dlogp), vec("entropy", entropy),
+        vec("dentropy", dentropy), gp, gstride, _stream_on(dev, stream))
+    _check(st, where)
+    return grad
 
 
 def _where_ptr(t):

@@ -53,6 +53,11 @@ struct DeviceBuf {
   template <typename T> T* as() const { return static_cast<T*>(p); }
 };
 
+struct RestoreDevice {
+  int device;
+  ~RestoreDevice() { cudaSetDevice(device); }
+};
+
 size_t storage_bytes(int dtype) { return dtype == XRL_BF16 ? 2 : 4; }
 
 }  // namespace
@@ -1269,6 +1274,51 @@ xrl_status xrl_gae(int32_t device, int32_t num_steps, int32_t num_trajectories, 
   XRL_CUDA(cudaSetDevice(device));
   launch_gae(reward, values, done, gamma, lambda, num_steps, num_trajectories, adv, ret,
              static_cast<cudaStream_t>(stream));
+  XRL_CUDA(cudaGetLastError());
+  return XRL_OK;
+}
+
+// A call that needs no context runs on its caller's device and leaves the thread's current device as it was.
+#define XRL_ON_DEVICE(device)                                  \
+  int previous_device = 0;                                     \
+  XRL_CUDA(cudaGetDevice(&previous_device));                   \
+  XRL_CUDA(cudaSetDevice(device));                             \
+  const RestoreDevice restore_device{previous_device}
+
+static bool logit_rows_ok(int32_t dtype, int32_t rows, int32_t vocab, const void* logits, int64_t row_stride,
+                          const uint8_t* mask, int64_t mask_stride, float scale) {
+  return (dtype == XRL_FP32 || dtype == XRL_BF16) && rows >= 0 && vocab >= 1 && scale > 0.f && scale <= 1e6f &&
+         (rows == 0 || logits) && reinterpret_cast<uintptr_t>(logits) % storage_bytes(dtype) == 0 &&
+         (rows <= 1 || row_stride >= vocab) && (!mask || rows <= 1 || mask_stride == 0 || mask_stride >= vocab);
+}
+
+xrl_status xrl_logprob(int32_t device, int32_t dtype, int32_t rows, int32_t vocab, const void* logits, int64_t row_stride,
+                       const int32_t* token, const uint8_t* mask, int64_t mask_stride, float scale, int32_t num_top,
+                       float* logp, float* entropy, float* norm, int32_t* top_token, float* top_logp, void* stream) {
+  if (!logit_rows_ok(dtype, rows, vocab, logits, row_stride, mask, mask_stride, scale)) return XRL_ERR_INVALID_ARG;
+  if (num_top < 0 || num_top > vocab || (rows > 0 && num_top > 0 && (!top_token || !top_logp)) ||
+      (rows > 0 && logp && !token) || reinterpret_cast<uintptr_t>(norm) % 8)
+    return XRL_ERR_INVALID_ARG;
+  if (num_top > XRL_MAX_TOP) return XRL_ERR_UNSUPPORTED;
+  XRL_ON_DEVICE(device);
+  launch_logprob(dtype, rows, vocab, logits, row_stride, token, mask, mask_stride, scale, num_top, logp, entropy, norm,
+                 top_token, top_logp, static_cast<cudaStream_t>(stream));
+  XRL_CUDA(cudaGetLastError());
+  return XRL_OK;
+}
+
+xrl_status xrl_logprob_grad(int32_t device, int32_t dtype, int32_t rows, int32_t vocab, const void* logits,
+                            int64_t row_stride, const int32_t* token, const uint8_t* mask, int64_t mask_stride, float scale,
+                            const float* norm, const float* dlogp, const float* entropy, const float* dentropy, void* grad,
+                            int64_t grad_stride, void* stream) {
+  if (!logit_rows_ok(dtype, rows, vocab, logits, row_stride, mask, mask_stride, scale)) return XRL_ERR_INVALID_ARG;
+  if ((rows > 0 && (!norm || !grad || (dlogp && !token) || (dentropy && !entropy))) || (rows > 1 && grad_stride < vocab) ||
+      reinterpret_cast<uintptr_t>(norm) % 8 || reinterpret_cast<uintptr_t>(grad) % storage_bytes(dtype) ||
+      (grad && grad == logits && rows > 1 && grad_stride != row_stride))
+    return XRL_ERR_INVALID_ARG;
+  XRL_ON_DEVICE(device);
+  launch_logprob_grad(dtype, rows, vocab, logits, row_stride, token, mask, mask_stride, scale, norm, dlogp, entropy, dentropy,
+                      grad, grad_stride, static_cast<cudaStream_t>(stream));
   XRL_CUDA(cudaGetLastError());
   return XRL_OK;
 }
