@@ -354,6 +354,33 @@ xrl_status xrl_logprob_grad(int32_t device, int32_t dtype, int32_t rows, int32_t
                             const float* norm, const float* dlogp, const float* entropy, const float* dentropy, void* grad,
                             int64_t grad_stride, void* stream);
 
+/* Orthogonalised updates (what the Muon optimiser applies in place of a matrix's gradient or momentum): the nearest
+ * matrix with singular values near 1, by Newton-Schulz products of the quintic
+ *   X = G / (||G||_F + eps);   `steps` times:  A = X X^T,  X <- 3.4445 X + (-4.7750 A + 2.0315 A^2) X
+ * (X^T X and products from the right for matrices with more rows than columns: the same in exact arithmetic).  Momentum,
+ * learning rate and the choice of matrices are the caller's.
+ *   dtype      XRL_FP32 or XRL_BF16, of G and of the result.  The products run on the tensor cores with fp32 accumulators:
+ *              for bf16 from operands of 11 bits with the diagonals of A and its polynomial kept in fp32 (an error of some
+ *              1e-3 of the result's norm before its rounding to bf16, which is 1.7e-3); for fp32 from operands of 22 bits
+ *   batch      matrices, batch_stride elements apart, rows row_stride apart (row_stride >= cols; the matrices must not
+ *              overlap); each side at most XRL_MAX_SIDE
+ *   steps      1 to 64 (5 is usual);   eps > 0 (1e-7 is usual): G = 0 gives 0, and so may a G whose norm is far below eps
+ *              (entries of X are kept to 2^-32 of the largest it can have)
+ *   out        laid out by its own strides; may be grad itself with the same strides
+ *   workspace  DEVICE, 256-byte aligned, of at least the bytes that xrl_orthogonalise_workspace says (HOST output; about 8 bytes
+ *              per entry of G and of the smaller Gram matrix).  It holds nothing between calls; calls that may run at the
+ *              same time need one each
+ *   device_status  DEVICE int32 [1] or NULL: XRL_OK, or XRL_ERR_TIMEOUT if a bounded wait ran out (the results are undefined then)
+ * A matrix with a NaN or an infinity becomes NaN; the others of its batch are not affected.  The results do not depend
+ * on anything but the inputs, bit for bit.  Needs no context; 2 + 3 * steps launches at most; captures into a CUDA graph.
+ * Errors: INVALID_ARG, UNSUPPORTED (sizes), CUDA. */
+#define XRL_MAX_SIDE 32768
+xrl_status xrl_orthogonalise_workspace(int32_t dtype, int32_t batch, int32_t rows, int32_t cols, size_t* bytes);
+xrl_status xrl_orthogonalise(int32_t device, int32_t dtype, int32_t batch, int32_t rows, int32_t cols, const void* grad,
+                             int64_t row_stride, int64_t batch_stride, int32_t steps, float eps, void* out,
+                             int64_t out_row_stride, int64_t out_batch_stride, void* workspace, size_t workspace_bytes,
+                             int32_t* device_status, void* stream);
+
 /* Data-parallel training step (Section 3.3.4: the objective is a mean over the environments of the mini-batch;
  * the paper leaves training on several devices as future work).  Every rank has run xrl_ppo_grad on its own
  * environments, so its gradient and loss terms are means over n_r local environments.  The mean over all

@@ -27,6 +27,7 @@ EXPORTED_SYMBOLS = [
     "xrl_profile", "xrl_profile_read", "xrl_pack_csr_static", "xrl_encode_delta", "xrl_delta_rows", "xrl_get_weights",
     "xrl_graph_begin", "xrl_graph_launch", "xrl_batch_set_edge_attr", "xrl_ppo_grad", "xrl_gae",
     "xrl_grad_weigh", "xrl_grad_unweigh", "xrl_init_weights", "xrl_round_features", "xrl_logprob", "xrl_logprob_grad",
+    "xrl_orthogonalise", "xrl_orthogonalise_workspace",
 ]
 PROFILE_FAMILIES = ["pack", "node_update", "transform", "aggregate", "readout", "heads", "aggregate_readout",
                     "layers_fused"]
@@ -95,6 +96,8 @@ def load_library():
         "xrl_ppo_grad": [vp] * 8 + [C.c_float] * 3 + [vp] * 4,
         "xrl_gae": [i32, i32, i32, vp, vp, vp, C.c_float, C.c_float, vp, vp, vp],
         "xrl_graph_launch": [vp, vp],
+        "xrl_orthogonalise_workspace": [i32, i32, i32, i32, C.POINTER(C.c_size_t)],
+        "xrl_orthogonalise": [i32, i32, i32, i32, i32, vp, i64, i64, i32, C.c_float, vp, i64, i64, vp, C.c_size_t, vp, vp],
         "xrl_logprob": [i32, i32, i32, i32, vp, i64, vp, vp, i64, C.c_float, i32] + [vp] * 6,
         "xrl_logprob_grad": [i32, i32, i32, i32, vp, i64, vp, vp, i64, C.c_float] + [vp] * 5 + [i64, vp],
         "xrl_grad_weigh": [i32, i32, i32, vp, i64, vp, i64, vp, vp],
@@ -438,6 +441,73 @@ def xrl_logprob_grad(logits, norm, token=None, dlogp=None, entropy=None, dentrop
         _flat(where, "norm", norm, "float32", rows, 2), vec("dlogp", dlogp), vec("entropy", entropy),
         vec("dentropy", dentropy), gp, gstride, _stream_on(dev, stream))
     _check(st, where)
+    return grad
+
+
+def xrl_orthogonalise_workspace(dtype, batch, rows, cols) -> int:
+    n = C.c_size_t()
+    _check(load_library().xrl_orthogonalise_workspace(dtype, batch, rows, cols, C.byref(n)), "xrl_orthogonalise_workspace")
+    return int(n.value)
+
+
+def _matrices_of(where, what, t, batch, rows, cols):
+    """(pointer, row stride, batch stride) of a [batch x rows x cols] or [rows x cols] tensor."""
+    if tuple(t.shape) != ((rows, cols) if t.dim() == 2 else (batch, rows, cols)) or (cols > 1 and t.stride(-1) != 1):
+        raise XrlError(1, f"{where} ({what}: [{batch} x {rows} x {cols}], entries of a row side by side)")
+    return t.data_ptr(), t.stride(-2) if rows > 1 else cols, t.stride(0) if t.dim() == 3 and batch > 1 else 0
+
+
+def xrl_orthogonalise(grad, steps=5, eps=1e-7, out=None, workspace=None, device_status=None, stream=None):
+    """Orthogonalised updates by Newton-Schulz products (see include/xrl.h).  grad: torch CUDA [rows, cols] or [batch, rows,
+    cols], float32 or bfloat16, entries of a row side by side; out: the same shape and type, may be grad itself, allocated
+    (contiguous) if None; workspace: uint8 tensor of xrl_orthogonalise_workspace bytes, allocated if None (on the call's
+    stream, so it is safe to let go); device_status: int32 [1] or None."""
+    where = "xrl_orthogonalise"
+    import torch
+    if grad.dim() not in (2, 3):
+        raise XrlError(1, f"{where} (grad: [rows x cols] or [batch x rows x cols])")
+    rows, cols = grad.shape[-2:]
+    batch = grad.shape[0] if grad.dim() == 3 else 1
+    dev = _device_of(where, grad, out, workspace, device_status)
+    dtype = _storage(where, grad)
+    if out is None:
+        out = torch.empty(grad.shape, dtype=grad.dtype, device=grad.device)
+    elif out.dtype != grad.dtype or out.dim() != grad.dim():
+        raise XrlError(1, f"{where} (out: type and shape of grad)")
+    gp, gld, gbs = _matrices_of(where, "grad", grad, batch, rows, cols)
+    op, old, obs = _matrices_of(where, "out", out, batch, rows, cols)
+    if workspace is None:
+        size = xrl_orthogonalise_workspace(dtype, batch, rows, cols)
+        if stream is None:
+            workspace = torch.empty(size, dtype=torch.uint8, device=grad.device)
+        else:
+            with torch.cuda.stream(torch.cuda.ExternalStream(int(stream), device=grad.device)):
+                workspace = torch.empty(size, dtype=torch.uint8, device=grad.device)
+    elif str(workspace.dtype) != "torch.uint8" or not workspace.is_contiguous():
+        raise XrlError(1, f"{where} (workspace: contiguous uint8)")
+    st = load_library().xrl_orthogonalise(
+        dev, dtype, batch, rows, cols, gp, gld, gbs, steps, eps, op, old, obs, workspace.data_ptr(), workspace.numel(),
+        _flat(where, "device_status", device_status, "int32", 1), _stream_on(dev, stream))
+    _check(st, where)
+    return out
+
+
+def layer_matrices(m, blob):
+    """The L attention layers' matrices W [H x H] of a weight or gradient blob, as a view [L, H, H] (model dict as for
+    model_config)."""
+    H, L = m["H"], m["L"]
+    first, apart = (2 * m["S"] + m["T"]) * H + H, H * H + 3 * H
+    return blob.as_strided((L, H, H), (apart, H, 1), blob.storage_offset() + first)
+
+
+def orthogonalise_layers(m, grad, steps=5, eps=1e-7, stream=None):
+    """In place: the layer matrices' part of an xrl_ppo_grad gradient becomes the orthogonalised update; the rest of the blob
+    stays the gradient."""
+    if grad.dim() != 1 or not grad.is_contiguous():
+        raise XrlError(1, "orthogonalise_layers (grad: a contiguous blob)")
+    if m["L"] > 0:
+        w = layer_matrices(m, grad)
+        xrl_orthogonalise(w, steps, eps, out=w, stream=stream)
     return grad
 
 

@@ -1323,6 +1323,44 @@ xrl_status xrl_logprob_grad(int32_t device, int32_t dtype, int32_t rows, int32_t
   return XRL_OK;
 }
 
+static xrl_status matrices_ok(int32_t dtype, int32_t batch, int32_t rows, int32_t cols) {
+  if ((dtype != XRL_FP32 && dtype != XRL_BF16) || batch < 0 || rows < 0 || cols < 0) return XRL_ERR_INVALID_ARG;
+  const int64_t tr = (int64_t(rows) + 127) / 128, tc = (int64_t(cols) + 127) / 128;
+  if (batch > 65535 || rows > XRL_MAX_SIDE || cols > XRL_MAX_SIDE || tr * tc * batch > INT32_MAX) return XRL_ERR_UNSUPPORTED;
+  return XRL_OK;
+}
+
+xrl_status xrl_orthogonalise_workspace(int32_t dtype, int32_t batch, int32_t rows, int32_t cols, size_t* bytes) {
+  const xrl_status ok = matrices_ok(dtype, batch, rows, cols);
+  if (ok != XRL_OK || !bytes) return ok != XRL_OK ? ok : XRL_ERR_INVALID_ARG;
+  *bytes = batch && rows && cols ? orthogonalise_workspace(batch, rows, cols) : 0;
+  return XRL_OK;
+}
+
+xrl_status xrl_orthogonalise(int32_t device, int32_t dtype, int32_t batch, int32_t rows, int32_t cols, const void* grad,
+                             int64_t row_stride, int64_t batch_stride, int32_t steps, float eps, void* out,
+                             int64_t out_row_stride, int64_t out_batch_stride, void* workspace, size_t workspace_bytes,
+                             int32_t* device_status, void* stream) {
+  const xrl_status ok = matrices_ok(dtype, batch, rows, cols);
+  if (ok != XRL_OK) return ok;
+  if (steps < 1 || steps > 64 || !(eps > 0.f) || std::isinf(eps)) return XRL_ERR_INVALID_ARG;
+  if (batch == 0 || rows == 0 || cols == 0) return XRL_OK;
+  const uintptr_t unit = storage_bytes(dtype);
+  auto strides_ok = [&](int64_t row, int64_t matrix) {
+    return (rows == 1 || row >= cols) && (batch == 1 || matrix >= int64_t(rows - 1) * (rows == 1 ? 0 : row) + cols);
+  };
+  if (!grad || !out || !workspace || reinterpret_cast<uintptr_t>(grad) % unit || reinterpret_cast<uintptr_t>(out) % unit ||
+      reinterpret_cast<uintptr_t>(workspace) % 256 || reinterpret_cast<uintptr_t>(device_status) % 4 ||
+      workspace_bytes < orthogonalise_workspace(batch, rows, cols) || !strides_ok(row_stride, batch_stride) ||
+      !strides_ok(out_row_stride, out_batch_stride))
+    return XRL_ERR_INVALID_ARG;
+  XRL_ON_DEVICE(device);
+  const bool done = launch_orthogonalise(dtype, batch, rows, cols, grad, row_stride, batch_stride, steps, eps, out, out_row_stride,
+                                         out_batch_stride, workspace, device_status, static_cast<cudaStream_t>(stream));
+  XRL_CUDA(cudaGetLastError());
+  return done ? XRL_OK : XRL_ERR_CUDA;
+}
+
 xrl_status xrl_grad_weigh(int32_t where, int32_t device, int32_t elem_bytes, const void* grad, int64_t count,
                           const void* loss, int64_t num_envs, void* buf, void* stream) {
   if ((where != XRL_MEM_HOST && where != XRL_MEM_DEVICE) || (elem_bytes != 4 && elem_bytes != 8) || count < 0 ||

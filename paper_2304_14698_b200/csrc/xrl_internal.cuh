@@ -292,6 +292,12 @@ int launch_logprob(int dtype, int64_t rows, int32_t vocab, const void* logits, i
 int launch_logprob_grad(int dtype, int64_t rows, int32_t vocab, const void* logits, int64_t row_stride, const int32_t* token,
                         const uint8_t* mask, int64_t mask_stride, float scale, const float* norm, const float* dlogp,
                         const float* entropy, const float* dentropy, void* grad, int64_t grad_stride, cudaStream_t st);
+// Newton-Schulz orthogonalisation; status: DEVICE word or null (one in the workspace).  False: a tensor map or an
+// attribute was refused.
+size_t orthogonalise_workspace(int32_t batch, int32_t rows, int32_t cols);
+bool launch_orthogonalise(int dtype, int32_t batch, int32_t rows, int32_t cols, const void* grad, int64_t ld, int64_t batch_stride,
+                          int32_t steps, float eps, void* out, int64_t out_ld, int64_t out_batch_stride, void* workspace,
+                          int32_t* status, cudaStream_t st);
 int launch_grad_weigh(int elem_bytes, const void* grad, int64_t count, const void* loss, int64_t n, void* buf,
                       cudaStream_t st);
 int launch_grad_unweigh(int elem_bytes, const void* buf, int64_t count, void* grad, void* loss, cudaStream_t st);
