@@ -29,25 +29,47 @@ namespace {
 
 constexpr float kA = 3.4445f, kB = -4.7750f, kC = 2.0315f;     // the quintic's coefficients
 constexpr float kGramScale = 16384.f;    // of F and of B's rest
-constexpr int kNormBlocks = 64;          // partial sums of squares per matrix, at most
+constexpr int kNormBlocks = 256;         // partial sums of squares per matrix, at most
 constexpr int kPad = 64;                 // row strides of the workspace's matrices are multiples of this
 
 struct Half2 { __half *hi, *lo; };
 
 // ---- norm and first X --------------------------------------------------------------------------------------------
+// eight entries of a row from column c on (0 beyond the last)
+template <typename T>
+__device__ __forceinline__ void load8(const T* row, int c, int cols, float (&f)[8]) {
+  constexpr int N = VecOf<T>::N;
+  if (c + 8 <= cols && (reinterpret_cast<uintptr_t>(row + c) & 15) == 0) {
+#pragma unroll
+    for (int i = 0; i < 8; i += N) {
+      float v[N];
+      unpack(*reinterpret_cast<const uint4*>(row + c + i), v);
+#pragma unroll
+      for (int t = 0; t < N; ++t) f[i + t] = v[t];
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = c + i < cols ? to_float(row[c + i]) : 0.f;
+  }
+}
+
 template <typename T>
 __global__ void __launch_bounds__(256)
-k_ns_norm(const T* __restrict__ g, int64_t ld, int64_t batch_stride, int rows, int cols, double* partial, int32_t* status) {
+k_ns_norm(const T* g, int64_t ld, int64_t batch_stride, int rows, int cols, double* partial, int32_t* status) {
   enter();
   __shared__ double red[8];
   const T* m = g + blockIdx.y * batch_stride;
   if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *status = XRL_OK;
+  const int groups = (cols + 7) / 8;
+  const int64_t pieces = int64_t(rows) * groups;
   double s = 0.0;
-  for (int r = blockIdx.x * 8 + (threadIdx.x >> 5); r < rows; r += gridDim.x * 8)
-    for (int c = threadIdx.x & 31; c < cols; c += 32) {
-      const double v = to_float(m[r * ld + c]);
-      s += v * v;
-    }
+  for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < pieces; i += int64_t(gridDim.x) * 256) {
+    const int64_t r = i / groups;
+    float f[8];
+    load8(m + r * ld, int(i - r * groups) * 8, cols, f);
+#pragma unroll
+    for (int t = 0; t < 8; ++t) s = fma(double(f[t]), double(f[t]), s);
+  }
 #pragma unroll
   for (int d = 16; d > 0; d >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, d);
   if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = s;
@@ -58,33 +80,45 @@ k_ns_norm(const T* __restrict__ g, int64_t ld, int64_t batch_stride, int rows, i
   }
 }
 
-__device__ __forceinline__ void split(float v, __half& hi, __half& lo) {
-  hi = __float2half_rn(v);
-  lo = __float2half_rn(v - __half2float(hi));
+// two values as hi + lo
+__device__ __forceinline__ void split2(float a, float b, uint32_t& hi, uint32_t& lo) {
+  const __half2 h = __floats2half2_rn(a, b);
+  const float2 back = __half22float2(h);
+  const __half2 l = __floats2half2_rn(a - back.x, b - back.y);
+  hi = *reinterpret_cast<const uint32_t*>(&h);
+  lo = *reinterpret_cast<const uint32_t*>(&l);
 }
 
 template <typename T>
 __global__ void __launch_bounds__(256)
-k_ns_start(const T* __restrict__ g, int64_t ld, int64_t batch_stride, int rows, int cols, const double* partial, int nparts,
-           double eps, float scale, Half2 x, int64_t ldx) {
+k_ns_start(const T* g, int64_t ld, int64_t batch_stride, int rows, int cols, const double* partial, int nparts, double eps,
+           float scale, Half2 x, int64_t ldx) {
   enter();
   __shared__ double s_inv;
-  if (threadIdx.x == 0) {
+  if (threadIdx.x < 32) {
     double s = 0.0;
-    for (int i = 0; i < nparts; ++i) s += partial[blockIdx.y * nparts + i];
-    s_inv = double(scale) / (sqrt(s) + eps);
+    for (int i = threadIdx.x; i < nparts; i += 32) s += partial[blockIdx.y * nparts + i];
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, d);
+    if (threadIdx.x == 0) s_inv = double(scale) / (sqrt(s) + eps);
   }
   __syncthreads();
   const double inv = s_inv;
   const T* m = g + blockIdx.y * batch_stride;
   const int64_t base = blockIdx.y * int64_t(rows) * ldx;
-  for (int r = blockIdx.x * 8 + (threadIdx.x >> 5); r < rows; r += gridDim.x * 8)
-    for (int c = threadIdx.x & 31; c < cols; c += 32) {
-      __half hi, lo;
-      split(float(double(to_float(m[r * ld + c])) * inv), hi, lo);
-      x.hi[base + r * ldx + c] = hi;
-      x.lo[base + r * ldx + c] = lo;
-    }
+  const int groups = (cols + 7) / 8;
+  const int64_t pieces = int64_t(rows) * groups;
+  for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < pieces; i += int64_t(gridDim.x) * 256) {
+    const int64_t r = i / groups;
+    const int c = int(i - r * groups) * 8;
+    float f[8];
+    load8(m + r * ld, c, cols, f);
+    uint32_t hi[4], lo[4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) split2(float(double(f[2 * t]) * inv), float(double(f[2 * t + 1]) * inv), hi[t], lo[t]);
+    *reinterpret_cast<uint4*>(x.hi + base + r * ldx + c) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+    *reinterpret_cast<uint4*>(x.lo + base + r * ldx + c) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+  }
 }
 
 // ---- the products ------------------------------------------------------------------------------------------------
@@ -107,27 +141,81 @@ struct NsArgs {
   int32_t* status;
 };
 
-constexpr int kTile = 128, kStep = 64;   // rows per CTA, reduction per stage
-constexpr int kOperand = kTile * kStep * 2;
+constexpr int kRows = 128, kStep = 64;   // rows of the result per CTA, reduction per stage
 constexpr int kEpiWarps = 8, kThreads = 64 + 32 * kEpiWarps;
+constexpr int kTurnPitch = 36;           // words per column of a warp's 32 x 16 piece that is being transposed
 
+// CTAS: of a tile.  A pair multiplies 256 rows by N columns with one instruction; each holds its 128 rows of the left operand
+// and N / 2 of the right one, so a tile of 256 x 256 asks half of what four of 128 x 128 do of L2.
 // CHUNK: stages whose products stay in one accumulator.  The tensor cores cut the sum after each instruction instead of
 // rounding it, which shrinks a sum of n instructions by about n / 4 units in its last place (fp32, 32 x 8,192 in one
 // accumulator: 4e-5 of the update).  fp32 updates therefore add the accumulators of 128 entries of the reduction in registers,
 // and issue the small products of a stage first, onto a small sum.
-template <int NPROD> struct Cfg {
+template <int CTAS, int NPROD> struct Cfg {
+  static constexpr int M = CTAS * kRows, N = CTAS == 2 && NPROD == 1 ? 256 : 128;
+  static constexpr int SUB = M / N;                       // tiles side by side in a square of M x M
   static constexpr int CHUNK = NPROD == 1 ? 1 << 30 : 2;
-  static constexpr int STAGE = kOperand * (NPROD == 1 ? 2 : 4);
-  static constexpr int STAGES = NPROD == 1 ? 6 : 3;
-  static constexpr int OFF_BAR = STAGES * STAGE;
+  static constexpr int B_ROWS = N / CTAS;
+  static constexpr int A_BYTES = kRows * kStep * 2, B_BYTES = B_ROWS * kStep * 2;
+  static constexpr int PARTS = NPROD == 1 ? 1 : 2;        // hi; hi and lo
+  static constexpr int OFF_B = PARTS * A_BYTES;           // a stage: A hi, A lo, B hi, B lo
+  static constexpr int STAGE = PARTS * (A_BYTES + B_BYTES);
+  static constexpr int STAGES = 192 * 1024 / STAGE;
+  static constexpr int OFF_TURN = STAGES * STAGE;
+  static constexpr int TURN_BYTES = 16 * kTurnPitch * 4;
+  static constexpr int OFF_BAR = OFF_TURN + kEpiWarps * TURN_BYTES;
   static constexpr int OFF_TMEM = OFF_BAR + 8 * (2 * STAGES + 4);
   static constexpr int SMEM_BYTES = OFF_TMEM + 16;
+  static constexpr int TMEM_COLS = 2 * N;
+  static_assert(SMEM_BYTES <= 227 * 1024, "shared memory of one SM");
 };
 
+// of a pair, every copy reports to the first CTA's barrier (the same offset; bit 24 of a shared address tells the two apart)
+template <int CTAS>
 __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
-  asm volatile(
-      "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
-      ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
+  if (CTAS == 1)
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+        ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
+  else
+    asm volatile(
+        "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+        ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar & 0xFEFFFFFFu) : "memory");
+}
+template <int CTAS>
+__device__ __forceinline__ void mma(uint32_t acc, uint64_t da, uint64_t db, uint32_t idesc, uint32_t add) {
+  if (CTAS == 1) {
+    tc_mma(acc, da, db, idesc, add);
+  } else {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+        ::"r"(acc), "l"(da), "l"(db), "r"(idesc), "r"(add) : "memory");
+  }
+}
+// arrives at the barrier, of a pair at both CTAs', when the products issued so far are done
+template <int CTAS> __device__ __forceinline__ void commit(uint32_t bar) {
+  if (CTAS == 1)
+    tc_commit(bar);
+  else
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+                 ::"r"(bar), "h"(uint16_t(3)) : "memory");
+}
+// arrives at the first CTA's barrier
+template <int CTAS> __device__ __forceinline__ void arrive_first(uint32_t bar) {
+  if (CTAS == 1) {
+    mbar_arrive(bar);
+  } else {
+    asm volatile(
+        "{\n\t.reg .b32 a;\n\t"
+        "mapa.shared::cluster.u32 a, %0, 0;\n\t"
+        "mbarrier.arrive.release.cluster.shared::cluster.b64 _, [a];\n\t}" ::"r"(bar) : "memory");
+  }
+}
+template <int CTAS> __device__ __forceinline__ void tile_sync() {      // all threads of the CTA, of a pair of both
+  if (CTAS == 1) __syncthreads();
+  else asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
 }
 // MN-major, 128-byte swizzle: 64 entries of the outer index by 8 of the reduction in 1,024 bytes, 64 x 64 chunks 8 KB apart
 __device__ __forceinline__ uint64_t smem_desc_mn(uint32_t addr) {
@@ -137,57 +225,73 @@ __device__ __forceinline__ uint64_t smem_desc_mn(uint32_t addr) {
 template <bool MN> __device__ __forceinline__ uint64_t operand_desc(uint32_t addr, int k) {
   return MN ? smem_desc_mn(addr + k * 2048) : smem_desc(addr + k * 32);
 }
-template <bool MN>
+template <int CTAS, bool MN, int ROWS>
 __device__ __forceinline__ void load_operand(uint32_t dst, const CUtensorMap* map, int outer, int k, int z, uint32_t bar) {
   if (MN) {
-    tma_load_3d(dst, map, outer, k, z, bar);
-    tma_load_3d(dst + kOperand / 2, map, outer + 64, k, z, bar);
+    for (int c = 0; c < ROWS; c += 64) tma_load_3d<CTAS>(dst + c * 128, map, outer + c, k, z, bar);
   } else {
-    tma_load_3d(dst, map, k, outer, z, bar);
+    tma_load_3d<CTAS>(dst, map, k, outer, z, bar);
   }
 }
 
-struct Tile { int z, i, j; };            // matrix, tile row, tile column
-template <bool SYM> __device__ __forceinline__ Tile tile_of(const NsArgs& a, int t) {
+// A tile: matrix, first row and column; `turned`: symmetric products store it a second time below the diagonal
+struct Tile { int z, row, col; bool turned; };
+template <int M, int N, bool SYM> __device__ __forceinline__ Tile tile_of(const NsArgs& a, int t) {
   Tile r;
   r.z = t / a.tiles;
   t -= r.z * a.tiles;
-  if (SYM) {                             // column by column of the upper triangle: column j holds j + 1 tiles
+  r.turned = false;
+  if (SYM) {                             // squares of M x M, column by column of the upper triangle: column j holds j + 1
+    const int sub = t % (M / N);
+    t /= M / N;
     int j = int((sqrtf(8.f * float(t) + 1.f) - 1.f) * 0.5f);
     while ((j + 1) * (j + 2) / 2 <= t) ++j;
     while (j * (j + 1) / 2 > t) --j;
-    r.j = j;
-    r.i = t - j * (j + 1) / 2;
+    const int i = t - j * (j + 1) / 2;
+    r.row = i * M;
+    r.col = j * M + sub * N;
+    r.turned = i != j;
   } else {
-    r.i = t / a.tiles_n;
-    r.j = t - r.i * a.tiles_n;
+    const int i = t / a.tiles_n;
+    r.row = i * M;
+    r.col = (t - i * a.tiles_n) * N;
   }
   return r;
 }
 
-__device__ __forceinline__ uint32_t pack_half2(__half a, __half b) {
-  return uint32_t(__half_as_ushort(a)) | (uint32_t(__half_as_ushort(b)) << 16);
+__device__ __forceinline__ void tc_ld16(uint32_t taddr, uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+        "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]) : "r"(taddr) : "memory");
 }
-__device__ __forceinline__ void load32(const __half* p, uint32_t (&r)[16]) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const uint4 v = *reinterpret_cast<const uint4*>(p + 8 * i);
-    r[4 * i] = v.x; r[4 * i + 1] = v.y; r[4 * i + 2] = v.z; r[4 * i + 3] = v.w;
-  }
+__device__ __forceinline__ void tc_st16(uint32_t taddr, const float* r) {
+  const uint32_t* u = reinterpret_cast<const uint32_t*>(r);
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};"
+      ::"r"(u[0]), "r"(u[1]), "r"(u[2]), "r"(u[3]), "r"(u[4]), "r"(u[5]), "r"(u[6]), "r"(u[7]), "r"(u[8]), "r"(u[9]),
+        "r"(u[10]), "r"(u[11]), "r"(u[12]), "r"(u[13]), "r"(u[14]), "r"(u[15]), "r"(taddr) : "memory");
 }
-__device__ __forceinline__ float half_of(const uint32_t (&r)[16], int i) {
-  return __half2float(__ushort_as_half(uint16_t(i & 1 ? r[i >> 1] >> 16 : r[i >> 1] & 0xFFFFu)));
+// 16 fp16 numbers
+__device__ __forceinline__ void load16(const __half* p, uint32_t (&r)[8]) {
+  const uint4 a = *reinterpret_cast<const uint4*>(p), b = *reinterpret_cast<const uint4*>(p + 8);
+  r[0] = a.x; r[1] = a.y; r[2] = a.z; r[3] = a.w;
+  r[4] = b.x; r[5] = b.y; r[6] = b.z; r[7] = b.w;
 }
-__device__ __forceinline__ void store_row(__half* p, const uint32_t (&r)[16]) {
+__device__ __forceinline__ void store16(__half* p, const uint32_t (&r)[8]) {
   store32(p, r[0], r[1], r[2], r[3], r[4], r[5], r[6], r[7]);
-  store32(p + 16, r[8], r[9], r[10], r[11], r[12], r[13], r[14], r[15]);
 }
-
-template <typename T> __device__ __forceinline__ void store_user(T* p, const float (&v)[32], int count) {
+__device__ __forceinline__ float2 floats_of(uint32_t hi, uint32_t lo) {
+  const float2 h = __half22float2(*reinterpret_cast<const __half2*>(&hi)), l = __half22float2(*reinterpret_cast<const __half2*>(&lo));
+  return make_float2(h.x + l.x, h.y + l.y);
+}
+template <typename T> __device__ __forceinline__ void store_user(T* p, const float (&v)[16], int count) {
   constexpr int N = VecOf<T>::N;
-  if (count == 32 && (reinterpret_cast<uintptr_t>(p) & 15) == 0) {
+  if (count >= 16 && (reinterpret_cast<uintptr_t>(p) & 15) == 0) {
 #pragma unroll
-    for (int i = 0; i < 32; i += N) {
+    for (int i = 0; i < 16; i += N) {
       float f[N];
 #pragma unroll
       for (int t = 0; t < N; ++t) f[t] = v[i + t];
@@ -195,106 +299,112 @@ template <typename T> __device__ __forceinline__ void store_user(T* p, const flo
     }
   } else {
 #pragma unroll
-    for (int i = 0; i < 32; ++i)
+    for (int i = 0; i < 16; ++i)
       if (i < count) p[i] = T(v[i]);
   }
 }
 
-// 32 columns of a row of the result, from the accumulator
+// What a warp reads beside the accumulator for 16 columns of its 32 rows; asked for one piece ahead
+struct Beside {
+  uint32_t hi[8], lo[8];
+};
+template <int MODE>
+__device__ __forceinline__ void ask(const NsArgs& a, int z, int row, int col, Beside& b) {
+  if (MODE == GRAM || row >= a.m || col >= a.n) return;
+  const int64_t at = (int64_t(z) * a.m + row) * a.ld_in + col;
+  load16(a.in.hi + at, b.hi);
+  load16(a.in.lo + at, b.lo);
+}
+// The next operand's 16 columns of a thread's row (a warp's 32 rows together) from the accumulator
 template <int MODE, bool TALL, int NPROD>
-__device__ __forceinline__ void finish(const NsArgs& a, const Tile& t, int row, int col, const float* v) {
+__device__ __forceinline__ void finish(const NsArgs& a, const Tile& t, int row, int col, int lane, const uint32_t (&v)[16],
+                                       const Beside& b, uint32_t* turn) {
   const int small = TALL ? a.n : a.m;                    // (symmetric products: both)
-  if (MODE == APPLY) {
-    if (row >= a.m || col >= a.n) return;
-    const int64_t at = (int64_t(t.z) * a.m + row) * a.ld_in + col;
-    uint32_t hi[16], lo[16];
-    load32(a.in.hi + at, hi);
-    load32(a.in.lo + at, lo);
-    float f[32];
-    const float* d = a.diag_in + int64_t(t.z) * small;
-    const float dr = TALL ? 0.f : kA + d[row];
+  if (col >= a.n) return;                                // all lanes
+  const bool in = row < a.m;
+  const float* d = a.diag_in + int64_t(t.z) * small;
+  float f[16];
+  if (MODE == GRAM) {
 #pragma unroll
-    for (int i = 0; i < 32; ++i) {
-      const float w = TALL ? kA + (col + i < small ? __ldg(d + col + i) : 0.f) : dr;
-      f[i] = fmaf(w, (half_of(hi, i) + half_of(lo, i)) * a.in_unscale, v[i] * a.descale);
+    for (int i = 0; i < 16; ++i) f[i] = __uint_as_float(v[i]) * a.descale;
+  } else {
+    const float dr = MODE == APPLY && TALL ? 0.f : in ? d[row] : 0.f;
+    float dc[16];
+    if (MODE == POLY || TALL) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) dc[i] = col + i < small ? __ldg(d + col + i) : 0.f;
     }
-    if (a.user) {
-      typedef typename std::conditional<NPROD == 1, bf16, float>::type T;
-      store_user(static_cast<T*>(a.user) + t.z * a.user_batch + row * a.user_ld + col, f, a.n - col < 32 ? a.n - col : 32);
-    } else {
 #pragma unroll
-      for (int i = 0; i < 32; i += 2) {
-        __half h0, h1, l0, l1;
-        split(f[i] * a.out_scale, h0, l0);
-        split(f[i + 1] * a.out_scale, h1, l1);
-        hi[i >> 1] = pack_half2(h0, h1);
-        lo[i >> 1] = pack_half2(l0, l1);
+    for (int i = 0; i < 16; i += 2) {
+      const float2 x = floats_of(b.hi[i >> 1], b.lo[i >> 1]);
+      const float x0 = x.x * a.in_unscale, x1 = x.y * a.in_unscale;
+      const float s0 = __uint_as_float(v[i]) * a.descale, s1 = __uint_as_float(v[i + 1]) * a.descale;
+      if (MODE == APPLY) {
+        f[i] = fmaf(kA + (TALL ? dc[i] : dr), x0, s0);
+        f[i + 1] = fmaf(kA + (TALL ? dc[i + 1] : dr), x1, s1);
+      } else {
+        f[i] = fmaf(kB, x0, kC * fmaf(dr + dc[i], x0, s0));
+        f[i + 1] = fmaf(kB, x1, kC * fmaf(dr + dc[i + 1], x1, s1));
       }
-      const int64_t to = (int64_t(t.z) * a.m + row) * a.ld_out + col;
-      store_row(a.out.hi + to, hi);
-      store_row(a.out.lo + to, lo);
     }
+  }
+  if (MODE != APPLY && !t.turned && in && row - col >= 0 && row - col < 16) {      // the diagonal, kept apart
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+      if (col + i == row) { s = MODE == GRAM ? f[i] : __uint_as_float(v[i]) * a.descale; f[i] = 0.f; }
+    if (MODE == POLY) { const float di = d[row]; s = fmaf(kB, di, kC * fmaf(di, di, s)); }
+    a.diag_out[int64_t(t.z) * small + row] = s;
+  }
+  if (MODE == APPLY && a.user) {
+    typedef typename std::conditional<NPROD == 1, bf16, float>::type T;
+    if (in) store_user(static_cast<T*>(a.user) + t.z * a.user_batch + row * a.user_ld + col, f, a.n - col);
     return;
   }
-  if (col >= a.n || row >= a.m) return;
-  float f[32];
-  const float* d = a.diag_in + int64_t(t.z) * small;
-  if (MODE == POLY) {
-    const int64_t at = (int64_t(t.z) * a.m + row) * a.ld_in + col;
-    uint32_t hi[16], lo[16];
-    load32(a.in.hi + at, hi);
-    load32(a.in.lo + at, lo);
-    const float di = d[row];
+  const bool lo_too = MODE != POLY || NPROD > 1;
+  uint32_t hi[8], lo[8];
 #pragma unroll
-    for (int i = 0; i < 32; ++i) {
-      const float x = (half_of(hi, i) + half_of(lo, i)) * a.in_unscale, dj = col + i < a.n ? __ldg(d + col + i) : 0.f;
-      const float s = v[i] * a.descale;
-      f[i] = col + i == row ? fmaf(kB, di, kC * fmaf(di, di, s)) : fmaf(kB, x, kC * fmaf(di + dj, x, s));
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 32; ++i) f[i] = v[i] * a.descale;
-  }
-  const bool lo_too = MODE == GRAM || NPROD > 1;
-  uint32_t hi[16], lo[16];
-#pragma unroll
-  for (int i = 0; i < 32; i += 2) {
-    __half h0, h1, l0, l1;
-#pragma unroll
-    for (int e = 0; e < 2; ++e)
-      if (col + i + e == row) { a.diag_out[int64_t(t.z) * small + row] = f[i + e]; f[i + e] = 0.f; }
-    split(f[i] * a.out_scale, h0, l0);
-    split(f[i + 1] * a.out_scale, h1, l1);
-    hi[i >> 1] = pack_half2(h0, h1);
-    lo[i >> 1] = pack_half2(l0, l1);
-  }
+  for (int i = 0; i < 8; ++i) split2(f[2 * i] * a.out_scale, f[2 * i + 1] * a.out_scale, hi[i], lo[i]);
   const int64_t base = int64_t(t.z) * a.m * a.ld_out;
-  store_row(a.out.hi + base + row * a.ld_out + col, hi);
-  if (lo_too) store_row(a.out.lo + base + row * a.ld_out + col, lo);
-  if (t.i != t.j) {                      // and below the diagonal: 32 lanes write 32 neighbours
+  if (in) {
+    store16(a.out.hi + base + row * a.ld_out + col, hi);
+    if (lo_too) store16(a.out.lo + base + row * a.ld_out + col, lo);
+  }
+  if (MODE != APPLY && t.turned) {                       // below the diagonal: lane l has half of column l / 2
+    __syncwarp();
 #pragma unroll
-    for (int i = 0; i < 32; ++i) {
-      if (col + i >= a.n) break;
-      const int64_t to = base + (col + i) * a.ld_out + row;
-      a.out.hi[to] = __ushort_as_half(uint16_t(i & 1 ? hi[i >> 1] >> 16 : hi[i >> 1]));
-      if (lo_too) a.out.lo[to] = __ushort_as_half(uint16_t(i & 1 ? lo[i >> 1] >> 16 : lo[i >> 1]));
+    for (int i = 0; i < 8; ++i) {
+      turn[(2 * i) * kTurnPitch + lane] = __byte_perm(hi[i], lo[i], 0x5410);
+      turn[(2 * i + 1) * kTurnPitch + lane] = __byte_perm(hi[i], lo[i], 0x7632);
+    }
+    __syncwarp();
+    const int c = lane >> 1, row0 = row - lane + (lane & 1) * 16;
+    const uint4* p = reinterpret_cast<const uint4*>(turn + c * kTurnPitch + (lane & 1) * 16);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint4 w = p[i];
+      hi[2 * i] = __byte_perm(w.x, w.y, 0x5410);
+      hi[2 * i + 1] = __byte_perm(w.z, w.w, 0x5410);
+      lo[2 * i] = __byte_perm(w.x, w.y, 0x7632);
+      lo[2 * i + 1] = __byte_perm(w.z, w.w, 0x7632);
+    }
+    if (col + c < a.n && row0 < a.ld_out) {              // (beyond m: into the padding)
+      store16(a.out.hi + base + (col + c) * a.ld_out + row0, hi);
+      if (lo_too) store16(a.out.lo + base + (col + c) * a.ld_out + row0, lo);
     }
   }
 }
 
 struct Maps { CUtensorMap a_hi, a_lo, b_hi, b_lo; };
 
-template <int MODE, bool TALL, int NPROD>
+template <int CTAS, int MODE, bool TALL, int NPROD>
 __global__ void __launch_bounds__(kThreads, 1) k_ns_product(const __grid_constant__ Maps maps, const NsArgs a) {
-  using C = Cfg<NPROD>;
+  using C = Cfg<CTAS, NPROD>;
   constexpr bool SYM = MODE != APPLY, A_MN = MODE == GRAM && TALL, B_MN = A_MN || (MODE == APPLY && !TALL);
   extern __shared__ __align__(1024) uint8_t smem[];
   const uint32_t base = smem_u32(smem);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  if ((base & 1023u) != 0) {
-    if (threadIdx.x == 0) raise(a.status, XRL_ERR_UNSUPPORTED);
-    return;
-  }
+  const int rank = int(blockIdx.x) % CTAS, first = int(blockIdx.x) / CTAS, step = int(gridDim.x) / CTAS;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + C::OFF_TMEM);
   auto bar_full = [&](int s) { return base + C::OFF_BAR + 8u * s; };
   auto bar_empty = [&](int s) { return base + C::OFF_BAR + 8u * (C::STAGES + s); };
@@ -302,19 +412,31 @@ __global__ void __launch_bounds__(kThreads, 1) k_ns_product(const __grid_constan
   auto bar_acc_empty = [&](int b) { return base + C::OFF_BAR + 8u * (2 * C::STAGES + 2 + b); };
   if (threadIdx.x == 0) {
     for (int s = 0; s < C::STAGES; ++s) { mbar_init(bar_full(s), 1); mbar_init(bar_empty(s), 1); }
-    for (int b = 0; b < 2; ++b) { mbar_init(bar_acc_full(b), 1); mbar_init(bar_acc_empty(b), kEpiWarps); }
+    for (int b = 0; b < 2; ++b) { mbar_init(bar_acc_full(b), 1); mbar_init(bar_acc_empty(b), CTAS * kEpiWarps); }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     fence_async_smem();
   }
   if (warp == 1) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
-                 ::"r"(smem_u32(tmem_slot)), "r"(uint32_t(2 * kTile)) : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    if (CTAS == 1) {
+      asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
+                   ::"r"(smem_u32(tmem_slot)), "r"(uint32_t(C::TMEM_COLS)) : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    } else {
+      asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;"
+                   ::"r"(smem_u32(tmem_slot)), "r"(uint32_t(C::TMEM_COLS)) : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
   }
   tc_fence_before();
-  __syncthreads();
+  __syncwarp();
+  tile_sync<CTAS>();
   tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
+  int total = a.total;
+  if ((base & 1023u) != 0) {             // the swizzle's pattern starts on 1,024 bytes
+    total = 0;
+    if (threadIdx.x == 0) raise(a.status, XRL_ERR_UNSUPPORTED);
+  }
   const int ksteps = (a.k + kStep - 1) / kStep;
   enter();
 
@@ -323,41 +445,42 @@ __global__ void __launch_bounds__(kThreads, 1) k_ns_product(const __grid_constan
       uint32_t it = 0;
       bool ok = true;
       fence_async_all();
-      for (int tile = blockIdx.x; ok && tile < a.total; tile += gridDim.x) {
-        const Tile t = tile_of<SYM>(a, tile);
+      for (int tile = first; ok && tile < total; tile += step) {
+        const Tile t = tile_of<C::M, C::N, SYM>(a, tile);
+        const int row = t.row + rank * kRows, col = t.col + rank * C::B_ROWS;
         for (int k = 0; k < ksteps; ++k, ++it) {
           const int s = it % C::STAGES;
           const uint32_t round = it / C::STAGES;
           if (round > 0 && !mbar_wait(bar_empty(s), (round - 1) & 1)) { ok = false; break; }
-          mbar_expect_tx(bar_full(s), C::STAGE);
+          if (rank == 0) mbar_expect_tx(bar_full(s), CTAS * C::STAGE);
           const uint32_t at = base + s * C::STAGE;
-          load_operand<A_MN>(at, &maps.a_hi, t.i * kTile, k * kStep, t.z, bar_full(s));
-          load_operand<B_MN>(at + kOperand, &maps.b_hi, t.j * kTile, k * kStep, t.z, bar_full(s));
+          load_operand<CTAS, A_MN, kRows>(at, &maps.a_hi, row, k * kStep, t.z, bar_full(s));
+          load_operand<CTAS, B_MN, C::B_ROWS>(at + C::OFF_B, &maps.b_hi, col, k * kStep, t.z, bar_full(s));
           if (NPROD > 1) {
-            load_operand<A_MN>(at + 2 * kOperand, &maps.a_lo, t.i * kTile, k * kStep, t.z, bar_full(s));
-            load_operand<B_MN>(at + 3 * kOperand, &maps.b_lo, t.j * kTile, k * kStep, t.z, bar_full(s));
+            load_operand<CTAS, A_MN, kRows>(at + C::A_BYTES, &maps.a_lo, row, k * kStep, t.z, bar_full(s));
+            load_operand<CTAS, B_MN, C::B_ROWS>(at + C::OFF_B + C::B_BYTES, &maps.b_lo, col, k * kStep, t.z, bar_full(s));
           }
         }
       }
-      if (!ok) {
+      if (!ok) {                         // the copies in flight land within microseconds of a wait that took seconds
         raise(a.status, XRL_ERR_TIMEOUT);
-        for (uint32_t j = it > uint32_t(C::STAGES) ? it - C::STAGES : 0; j < it; ++j)
-          mbar_wait(bar_full(j % C::STAGES), (j / C::STAGES) & 1);
+        const unsigned long long t0 = now_ns();
+        while (now_ns() - t0 < 5000000ull) {}
       }
     }
   } else if (warp == 1) {
-    if (lane == 0) {
-      // fp32 accumulators, fp16 x fp16, M = N = 128; bits 15 and 16: MN-major operands
-      constexpr uint32_t idesc = (1u << 4) | (A_MN ? 1u << 15 : 0u) | (B_MN ? 1u << 16 : 0u) | (uint32_t(kTile >> 3) << 17) |
-                                 (uint32_t(kTile >> 4) << 24);
+    if (lane == 0 && rank == 0) {
+      // fp32 accumulators, fp16 x fp16; bits 15 and 16: MN-major operands
+      constexpr uint32_t idesc = (1u << 4) | (A_MN ? 1u << 15 : 0u) | (B_MN ? 1u << 16 : 0u) | (uint32_t(C::N >> 3) << 17) |
+                                 (uint32_t(C::M >> 4) << 24);
       uint32_t it = 0, lt = 0;
       bool ok = true;
-      for (int tile = blockIdx.x; ok && tile < a.total; tile += gridDim.x) {
+      for (int tile = first; ok && tile < total; tile += step) {
         for (int k0 = 0; ok && k0 < ksteps; k0 = k0 < ksteps - C::CHUNK ? k0 + C::CHUNK : ksteps, ++lt) {
           const int k1 = k0 < ksteps - C::CHUNK ? k0 + C::CHUNK : ksteps, buf = lt & 1;
           if (lt > 1 && !mbar_wait(bar_acc_empty(buf), ((lt >> 1) - 1) & 1)) { ok = false; break; }
           tc_fence_after();
-          const uint32_t acc = tmem_base + uint32_t(buf * kTile);
+          const uint32_t acc = tmem_base + uint32_t(buf * C::N);
           for (int k = k0; k < k1; ++k, ++it) {
             const int s = it % C::STAGES;
             if (!mbar_wait(bar_full(s), (it / C::STAGES) & 1)) { ok = false; break; }
@@ -366,32 +489,36 @@ __global__ void __launch_bounds__(kThreads, 1) k_ns_product(const __grid_constan
             if (NPROD > 1) {
 #pragma unroll
               for (int kk = 0; kk < kStep / 16; ++kk) {
-                tc_mma(acc, operand_desc<A_MN>(at, kk), operand_desc<B_MN>(at + 3 * kOperand, kk), idesc, k > k0 || kk ? 1u : 0u);
-                tc_mma(acc, operand_desc<A_MN>(at + 2 * kOperand, kk), operand_desc<B_MN>(at + kOperand, kk), idesc, 1u);
+                mma<CTAS>(acc, operand_desc<A_MN>(at, kk), operand_desc<B_MN>(at + C::OFF_B + C::B_BYTES, kk), idesc,
+                          k > k0 || kk ? 1u : 0u);
+                mma<CTAS>(acc, operand_desc<A_MN>(at + C::A_BYTES, kk), operand_desc<B_MN>(at + C::OFF_B, kk), idesc, 1u);
               }
             }
 #pragma unroll
             for (int kk = 0; kk < kStep / 16; ++kk)
-              tc_mma(acc, operand_desc<A_MN>(at, kk), operand_desc<B_MN>(at + kOperand, kk), idesc,
-                     NPROD > 1 || k > k0 || kk ? 1u : 0u);
-            tc_commit(bar_empty(s));
+              mma<CTAS>(acc, operand_desc<A_MN>(at, kk), operand_desc<B_MN>(at + C::OFF_B, kk), idesc,
+                        NPROD > 1 || k > k0 || kk ? 1u : 0u);
+            commit<CTAS>(bar_empty(s));
           }
-          if (ok) tc_commit(bar_acc_full(buf));
+          if (ok) commit<CTAS>(bar_acc_full(buf));
         }
       }
       if (!ok) raise(a.status, XRL_ERR_TIMEOUT);
     }
   } else {
-    constexpr int COLS = kTile / 2;      // of a warp
+    constexpr int COLS = C::N / 2;       // of a warp
     const int q = warp & 3, half = (warp - 2) >> 2;
+    uint32_t* turn = reinterpret_cast<uint32_t*>(smem + C::OFF_TURN + (warp - 2) * C::TURN_BYTES);
     uint32_t lt = 0;
     bool ok = true;
-    for (int tile = blockIdx.x; ok && tile < a.total; tile += gridDim.x) {
-      const Tile t = tile_of<SYM>(a, tile);
-      const int row = t.i * kTile + q * 32 + lane, col = t.j * kTile + half * COLS;
+    for (int tile = first; ok && tile < total; tile += step) {
+      const Tile t = tile_of<C::M, C::N, SYM>(a, tile);
+      const int row = t.row + rank * kRows + q * 32 + lane, col = t.col + half * COLS;
+      Beside next;
+      ask<MODE>(a, t.z, row, col, next);
       float sum[NPROD == 1 ? 1 : COLS];
-      for (int k0 = 0; k0 < ksteps; k0 = k0 < ksteps - C::CHUNK ? k0 + C::CHUNK : ksteps, ++lt) {
-        const int buf = lt & 1;
+      for (int k0 = 0; k0 < ksteps; ++lt) {
+        const int k1 = k0 < ksteps - C::CHUNK ? k0 + C::CHUNK : ksteps, buf = lt & 1;
         uint32_t got = 1;
         if (lane == 0) {
           got = 0;                       // a whole tile is multiplied first: the limit of one wait, several times over
@@ -401,46 +528,54 @@ __global__ void __launch_bounds__(kThreads, 1) k_ns_product(const __grid_constan
         ok = __shfl_sync(0xFFFFFFFFu, got, 0) != 0;
         if (!ok) break;
         tc_fence_after();
-        const uint32_t taddr = tmem_base + (uint32_t(q * 32) << 16) + uint32_t(buf * kTile + half * COLS);
-        if (NPROD == 1) {                // straight from the accumulator
-#pragma unroll 1
-          for (int c = 0; c < COLS; c += 32) {
-            __syncwarp();
-            uint32_t v[32];
-            tc_ld32(taddr + c, v);
-            tc_wait_ld();
-            float f[32];
+        const uint32_t taddr = tmem_base + (uint32_t(q * 32) << 16) + uint32_t(buf * C::N + half * COLS);
+        if (NPROD > 1 && ksteps > C::CHUNK) {
+          // the sums so far; with the last accumulator they go back into its place
 #pragma unroll
-            for (int i = 0; i < 32; ++i) f[i] = __uint_as_float(v[i]);
-            finish<MODE, TALL, NPROD>(a, t, row, col + c, f);
+          for (int c = 0; c < COLS; c += 16) {
+            uint32_t v[16];
+            tc_ld16(taddr + c, v);
+            tc_wait_ld();
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              float& x = sum[NPROD == 1 ? 0 : c + i];
+              x = (k0 == 0 ? 0.f : x) + __uint_as_float(v[i]);
+            }
           }
-        } else {
+          if (k1 == ksteps) {
 #pragma unroll
-          for (int c = 0; c < COLS; c += 32) {
-            uint32_t v[32];
-            tc_ld32(taddr + c, v);
+            for (int c = 0; c < COLS; c += 16) tc_st16(taddr + c, sum + (NPROD == 1 ? 0 : c));
+            asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+          }
+        }
+        if (k1 == ksteps) {
+#pragma unroll 1
+          for (int c = 0; c < COLS; c += 16) {
+            const Beside beside = next;
+            if (c + 16 < COLS) ask<MODE>(a, t.z, row, col + c + 16, next);
+            __syncwarp();
+            uint32_t v[16];
+            tc_ld16(taddr + c, v);
             tc_wait_ld();
-#pragma unroll
-            for (int i = 0; i < 32; ++i) sum[NPROD == 1 ? 0 : c + i] = (k0 == 0 ? 0.f : sum[NPROD == 1 ? 0 : c + i]) + __uint_as_float(v[i]);
+            finish<MODE, TALL, NPROD>(a, t, row, col + c, lane, v, beside, turn);
           }
         }
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(bar_acc_empty(buf));
+        if (lane == 0) arrive_first<CTAS>(bar_acc_empty(buf));
+        k0 = k1;
       }
-      if (!ok) break;
-      if (NPROD > 1) {
-#pragma unroll
-        for (int c = 0; c < COLS; c += 32) finish<MODE, TALL, NPROD>(a, t, row, col + c, sum + c);
-      }
-      __syncwarp();
     }
   }
   tc_fence_before();
-  __syncthreads();
+  __syncwarp();
+  tile_sync<CTAS>();
   if (warp == 1) {
     tc_fence_after();
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(uint32_t(2 * kTile)) : "memory");
+    if (CTAS == 1)
+      asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(uint32_t(C::TMEM_COLS)) : "memory");
+    else
+      asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(uint32_t(C::TMEM_COLS)) : "memory");
   }
 }
 
@@ -457,19 +592,36 @@ bool make_map3(CUtensorMap* m, const void* ptr, int batch, int rows, int cols, i
             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
-// one operand's pair of maps: its outer index along the rows (K-major) or along the columns (MN-major)
-bool make_operand(CUtensorMap* hi, CUtensorMap* lo, const Half2& p, int batch, int rows, int cols, int64_t ld, bool mn) {
-  const uint32_t box = mn ? kStep : kTile;
+// one operand's pair of maps: its outer index along the rows (K-major, `outer` of them a load) or along the columns (MN-major)
+bool make_operand(CUtensorMap* hi, CUtensorMap* lo, const Half2& p, int batch, int rows, int cols, int64_t ld, bool mn, int outer) {
+  const uint32_t box = mn ? kStep : outer;
   return make_map3(hi, p.hi, batch, rows, cols, ld, box) && make_map3(lo, p.lo, batch, rows, cols, ld, box);
 }
 
-template <int MODE, bool TALL, int NPROD>
-bool launch_product(const Maps& maps, const NsArgs& a, cudaStream_t st) {
+template <int CTAS, int MODE, bool TALL, int NPROD>
+bool launch_product(const Maps& maps, NsArgs a, int batch, cudaStream_t st) {
+  using C = Cfg<CTAS, NPROD>;
   static bool done[64] = {};
-  if (!ensure_dynamic_smem(k_ns_product<MODE, TALL, NPROD>, Cfg<NPROD>::SMEM_BYTES, done)) return false;
-  const unsigned grid = unsigned(a.total < kNumSMs ? a.total : kNumSMs);
-  launch(k_ns_product<MODE, TALL, NPROD>, grid, kThreads, Cfg<NPROD>::SMEM_BYTES, st, maps, a);
-  return true;
+  if (!ensure_dynamic_smem(k_ns_product<CTAS, MODE, TALL, NPROD>, C::SMEM_BYTES, done)) return false;
+  const int tm = (a.m + C::M - 1) / C::M;
+  a.tiles_n = (a.n + C::N - 1) / C::N;
+  a.tiles = MODE == APPLY ? tm * a.tiles_n : tm * (tm + 1) / 2 * C::SUB;
+  a.total = a.tiles * batch;
+  const int most = kNumSMs / CTAS;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = unsigned((a.total < most ? a.total : most) * CTAS);
+  cfg.blockDim = kThreads;
+  cfg.dynamicSmemBytes = C::SMEM_BYTES;
+  cfg.stream = st;
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  at[1].id = cudaLaunchAttributeClusterDimension;
+  at[1].val.clusterDim.x = CTAS;
+  at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = CTAS > 1 ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, k_ns_product<CTAS, MODE, TALL, NPROD>, maps, a) == cudaSuccess;
 }
 
 // the workspace's pieces
@@ -509,24 +661,22 @@ NsSpace layout(void* ws, int batch, int rows, int cols) {
   return s;
 }
 
-template <typename T, int NPROD, bool TALL>
+template <typename T, int NPROD, bool TALL, int CTAS>
 bool run_steps(int batch, int rows, int cols, const void* grad, int64_t ld, int64_t bs, int steps, double eps, void* out,
                int64_t out_ld, int64_t out_bs, const NsSpace& s, int32_t* status, cudaStream_t st) {
+  using C = Cfg<CTAS, NPROD>;
   const int small = TALL ? cols : rows, large = TALL ? rows : cols;
   int k = int(lround(0.5 * log2(double(rows) * double(cols))));
   if (k > 14) k = 14;
   const float xs = float(1 << k);
-  const int rb = (rows + 7) / 8 < kNormBlocks ? (rows + 7) / 8 : kNormBlocks;
-  launch(k_ns_norm<T>, dim3(rb, batch), 256, 0, st, static_cast<const T*>(grad), ld, bs, rows, cols, s.partial, status);
-  launch(k_ns_start<T>, dim3((rows + 7) / 8, batch), 256, 0, st, static_cast<const T*>(grad), ld, bs, rows, cols, s.partial, rb,
-         eps, xs, s.x[0], s.ldx);
+  const int64_t pieces = (int64_t(rows) * ((cols + 7) / 8) + 255) / 256;
+  const int nb = int(pieces < kNormBlocks ? pieces : kNormBlocks), sb = int(pieces < 8 * kNumSMs ? pieces : 8 * kNumSMs);
+  launch(k_ns_norm<T>, dim3(nb, batch), 256, 0, st, static_cast<const T*>(grad), ld, bs, rows, cols, s.partial, status);
+  launch(k_ns_start<T>, dim3(sb, batch), 256, 0, st, static_cast<const T*>(grad), ld, bs, rows, cols, s.partial, nb, eps, xs,
+         s.x[0], s.ldx);
 
-  const int tm = (small + kTile - 1) / kTile, tl = (large + kTile - 1) / kTile;
   NsArgs sym = {};
   sym.m = sym.n = small;
-  sym.tiles_n = tm;
-  sym.tiles = tm * (tm + 1) / 2;
-  sym.total = sym.tiles * batch;
   sym.ld_in = sym.ld_out = s.ldm;
   sym.out_scale = kGramScale;
   sym.in_unscale = 1.f / kGramScale;
@@ -545,9 +695,6 @@ bool run_steps(int batch, int rows, int cols, const void* grad, int64_t ld, int6
   apply.m = rows;
   apply.n = cols;
   apply.k = small;
-  apply.tiles_n = TALL ? tm : tl;
-  apply.tiles = tm * tl;
-  apply.total = apply.tiles * batch;
   apply.descale = 1.f / (kGramScale * xs);
   apply.ld_in = apply.ld_out = s.ldx;
   apply.in_unscale = 1.f / xs;
@@ -555,20 +702,17 @@ bool run_steps(int batch, int rows, int cols, const void* grad, int64_t ld, int6
   apply.diag_in = s.dB;
 
   Maps mg[2], mp, ma[2];
-  bool ok = make_operand(&mp.a_hi, &mp.a_lo, s.f, batch, small, small, s.ldm, false);
-  mp.b_hi = mp.a_hi;
-  mp.b_lo = mp.a_lo;
+  bool ok = make_operand(&mp.a_hi, &mp.a_lo, s.f, batch, small, small, s.ldm, false, kRows) &&
+            make_operand(&mp.b_hi, &mp.b_lo, s.f, batch, small, small, s.ldm, false, C::B_ROWS);
   for (int i = 0; i < 2; ++i) {
-    ok = ok && make_operand(&mg[i].a_hi, &mg[i].a_lo, s.x[i], batch, rows, cols, s.ldx, TALL);
-    mg[i].b_hi = mg[i].a_hi;
-    mg[i].b_lo = mg[i].a_lo;
-    if (TALL) {
-      ok = ok && make_operand(&ma[i].a_hi, &ma[i].a_lo, s.x[i], batch, rows, cols, s.ldx, false) &&
-           make_operand(&ma[i].b_hi, &ma[i].b_lo, s.b, batch, small, small, s.ldm, false);
-    } else {
-      ok = ok && make_operand(&ma[i].a_hi, &ma[i].a_lo, s.b, batch, small, small, s.ldm, false) &&
-           make_operand(&ma[i].b_hi, &ma[i].b_lo, s.x[i], batch, rows, cols, s.ldx, true);
-    }
+    ok = ok && make_operand(&mg[i].a_hi, &mg[i].a_lo, s.x[i], batch, rows, cols, s.ldx, TALL, kRows) &&
+         make_operand(&mg[i].b_hi, &mg[i].b_lo, s.x[i], batch, rows, cols, s.ldx, TALL, C::B_ROWS);
+    if (TALL)
+      ok = ok && make_operand(&ma[i].a_hi, &ma[i].a_lo, s.x[i], batch, rows, cols, s.ldx, false, kRows) &&
+           make_operand(&ma[i].b_hi, &ma[i].b_lo, s.b, batch, small, small, s.ldm, false, C::B_ROWS);
+    else
+      ok = ok && make_operand(&ma[i].a_hi, &ma[i].a_lo, s.b, batch, small, small, s.ldm, false, kRows) &&
+           make_operand(&ma[i].b_hi, &ma[i].b_lo, s.x[i], batch, rows, cols, s.ldx, true, C::B_ROWS);
   }
   for (int i = 0; ok && i < steps; ++i) {
     apply.in = s.x[i & 1];
@@ -578,10 +722,17 @@ bool run_steps(int batch, int rows, int cols, const void* grad, int64_t ld, int6
       apply.user_ld = out_ld;
       apply.user_batch = out_bs;
     }
-    ok = launch_product<GRAM, TALL, NPROD>(mg[i & 1], gram, st) && launch_product<POLY, false, NPROD>(mp, poly, st) &&
-         launch_product<APPLY, TALL, NPROD>(ma[i & 1], apply, st);
+    ok = launch_product<CTAS, GRAM, TALL, NPROD>(mg[i & 1], gram, batch, st) &&
+         launch_product<CTAS, POLY, false, NPROD>(mp, poly, batch, st) &&
+         launch_product<CTAS, APPLY, TALL, NPROD>(ma[i & 1], apply, batch, st);
   }
   return ok;
+}
+
+// Pairs of CTAs where their tiles of the square product keep most SMs busy
+bool pairs(int batch, int rows, int cols, int columns) {
+  const int64_t tiles = (int64_t(rows) + 255) / 256 * ((int64_t(cols) + columns - 1) / columns) * batch;
+  return tiles >= 60;
 }
 
 }  // namespace
@@ -593,8 +744,12 @@ bool launch_orthogonalise(int dtype, int32_t batch, int32_t rows, int32_t cols, 
                           int32_t* status, cudaStream_t st) {
   const NsSpace s = layout(workspace, batch, rows, cols);
   if (!status) status = s.status;
-  auto f = dtype == XRL_BF16 ? (rows > cols ? run_steps<bf16, 1, true> : run_steps<bf16, 1, false>)
-                             : (rows > cols ? run_steps<float, 3, true> : run_steps<float, 3, false>);
+  const bool bf = dtype == XRL_BF16, tall = rows > cols;
+  auto f = pairs(batch, rows, cols, bf ? 256 : 128)
+               ? (bf ? (tall ? run_steps<bf16, 1, true, 2> : run_steps<bf16, 1, false, 2>)
+                     : (tall ? run_steps<float, 3, true, 2> : run_steps<float, 3, false, 2>))
+               : (bf ? (tall ? run_steps<bf16, 1, true, 1> : run_steps<bf16, 1, false, 1>)
+                     : (tall ? run_steps<float, 3, true, 1> : run_steps<float, 3, false, 1>));
   return f(batch, rows, cols, grad, ld, batch_stride, steps, double(eps), out, out_ld, out_batch_stride, s, status, st);
 }
 

@@ -47,7 +47,7 @@ def make(dtype, *shape, seed=0, kind="gradient"):
 
 
 SHAPES = [(1, 1), (1, 7), (7, 1), (2, 3), (8, 8), (33, 31), (64, 64), (127, 129), (129, 127), (128, 128), (200, 136), (56, 256),
-          (256, 256), (100, 1000), (1000, 100), (512, 512), (385, 513), (513, 385), (1024, 640), (640, 1025), (1500, 1500), (32, 8192)]
+          (256, 256), (100, 1000), (1000, 100), (512, 512), (385, 513), (513, 385), (1024, 640), (640, 1025), (1500, 1500), (32, 8192), (2070, 2500), (2500, 2070)]
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
