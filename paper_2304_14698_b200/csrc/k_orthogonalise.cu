@@ -128,21 +128,21 @@ struct NsArgs {
   int tiles_n, tiles;                    // per matrix; symmetric products: tiles on and above the diagonal
   int total;                             // tiles of all matrices
   float descale;                         // accumulator -> value
-  Half2 in;                              // POLY: F; APPLY: X (the product's shape)
+  float gain;                            // accumulator -> its share of the scaled result
+  Half2 in;                              // POLY: F; APPLY: X (the product's shape and the result's scale)
   int64_t ld_in;
-  float in_unscale;
   const float* diag_in;                  // [batch x small side]
   Half2 out;
   int64_t ld_out;
-  float out_scale;
   float* diag_out;
   void* user;                            // APPLY: the caller's matrices in place of `out`
   int64_t user_ld, user_batch;
+  float unscale;                         // scaled result -> the caller's
   int32_t* status;
 };
 
 constexpr int kRows = 128, kStep = 64;   // rows of the result per CTA, reduction per stage
-constexpr int kEpiWarps = 8, kThreads = 64 + 32 * kEpiWarps;
+constexpr int kEpiWarps = 16, kThreads = 64 + 32 * kEpiWarps;
 constexpr int kTurnPitch = 36;           // words per column of a warp's 32 x 16 piece that is being transposed
 
 // CTAS: of a tile.  A pair multiplies 256 rows by N columns with one instruction; each holds its 128 rows of the left operand
@@ -151,8 +151,8 @@ constexpr int kTurnPitch = 36;           // words per column of a warp's 32 x 16
 // rounding it, which shrinks a sum of n instructions by about n / 4 units in its last place (fp32, 32 x 8,192 in one
 // accumulator: 4e-5 of the update).  fp32 updates therefore add the accumulators of 128 entries of the reduction in registers,
 // and issue the small products of a stage first, onto a small sum.
-template <int CTAS, int NPROD> struct Cfg {
-  static constexpr int M = CTAS * kRows, N = CTAS == 2 && NPROD == 1 ? 256 : 128;
+template <int CTAS, int COLS, int NPROD> struct Cfg {
+  static constexpr int M = CTAS * kRows, N = COLS;
   static constexpr int SUB = M / N;                       // tiles side by side in a square of M x M
   static constexpr int CHUNK = NPROD == 1 ? 1 << 30 : 2;
   static constexpr int B_ROWS = N / CTAS;
@@ -160,14 +160,15 @@ template <int CTAS, int NPROD> struct Cfg {
   static constexpr int PARTS = NPROD == 1 ? 1 : 2;        // hi; hi and lo
   static constexpr int OFF_B = PARTS * A_BYTES;           // a stage: A hi, A lo, B hi, B lo
   static constexpr int STAGE = PARTS * (A_BYTES + B_BYTES);
-  static constexpr int STAGES = 192 * 1024 / STAGE;
+  static constexpr int STAGES = 184 * 1024 / STAGE < 6 ? 184 * 1024 / STAGE : 6;
   static constexpr int OFF_TURN = STAGES * STAGE;
   static constexpr int TURN_BYTES = 16 * kTurnPitch * 4;
   static constexpr int OFF_BAR = OFF_TURN + kEpiWarps * TURN_BYTES;
   static constexpr int OFF_TMEM = OFF_BAR + 8 * (2 * STAGES + 4);
   static constexpr int SMEM_BYTES = OFF_TMEM + 16;
   static constexpr int TMEM_COLS = 2 * N;
-  static_assert(SMEM_BYTES <= 227 * 1024, "shared memory of one SM");
+  static constexpr int WARP_COLS = N / (kEpiWarps / 4);   // of an epilogue warp
+  static_assert(SMEM_BYTES <= 227 * 1024 && M % N == 0 && WARP_COLS % 16 == 0, "shared memory of one SM, whole squares");
 };
 
 // of a pair, every copy reports to the first CTA's barrier (the same offset; bit 24 of a shared address tells the two apart)
@@ -304,71 +305,85 @@ template <typename T> __device__ __forceinline__ void store_user(T* p, const flo
   }
 }
 
-// What a warp reads beside the accumulator for 16 columns of its 32 rows; asked for one piece ahead
-struct Beside {
-  uint32_t hi[8], lo[8];
+// An epilogue warp's part of a tile: 32 rows, a lane each, by 16 columns at a time
+struct Piece {
+  bool in, diag;                         // the row is the matrix's; the warp's part can hold diagonal entries
+  int row;
+  int64_t in_at, out_at, turn_at;        // of the lane's row in `in` and `out`; of its half column below the diagonal
+  const float* d;                        // diagonal of the matrix
+  float dr;                              // the row's own
 };
-template <int MODE>
-__device__ __forceinline__ void ask(const NsArgs& a, int z, int row, int col, Beside& b) {
-  if (MODE == GRAM || row >= a.m || col >= a.n) return;
-  const int64_t at = (int64_t(z) * a.m + row) * a.ld_in + col;
-  load16(a.in.hi + at, b.hi);
-  load16(a.in.lo + at, b.lo);
+template <int MODE, bool TALL>
+__device__ __forceinline__ Piece piece_of(const NsArgs& a, const Tile& t, int row, int col, int lane) {
+  Piece p;
+  p.row = row;
+  p.in = row < a.m;
+  p.diag = MODE != APPLY && !t.turned && row - lane < col + 256 && col < row - lane + 32;
+  const int64_t r = int64_t(t.z) * a.m + row;
+  p.in_at = r * a.ld_in + col;
+  p.out_at = r * a.ld_out + col;
+  p.turn_at = (int64_t(t.z) * a.m + col + (lane >> 1)) * a.ld_out + (row - lane + (lane & 1) * 16);
+  p.d = a.diag_in + int64_t(t.z) * (TALL ? a.n : a.m);
+  p.dr = MODE == GRAM || (MODE == APPLY && TALL) || !p.in ? 0.f : p.d[row];
+  return p;
 }
-// The next operand's 16 columns of a thread's row (a warp's 32 rows together) from the accumulator
+struct Beside { uint32_t hi[8], lo[8]; };                // 16 entries of `in`
+template <int MODE>
+__device__ __forceinline__ void ask(const NsArgs& a, const Piece& p, int col, int c, Beside& b) {
+  if (MODE == GRAM || !p.in || col + c >= a.n) return;
+  load16(a.in.hi + p.in_at + c, b.hi);
+  load16(a.in.lo + p.in_at + c, b.lo);
+}
+// Columns col + c ... + 15 of the next operand from the accumulator's v
 template <int MODE, bool TALL, int NPROD>
-__device__ __forceinline__ void finish(const NsArgs& a, const Tile& t, int row, int col, int lane, const uint32_t (&v)[16],
-                                       const Beside& b, uint32_t* turn) {
-  const int small = TALL ? a.n : a.m;                    // (symmetric products: both)
+__device__ __forceinline__ void finish(const NsArgs& a, const Tile& t, const Piece& p, int col0, int c, int lane,
+                                       const uint32_t (&v)[16], const Beside& b, uint32_t* turn) {
+  const int col = col0 + c;
   if (col >= a.n) return;                                // all lanes
-  const bool in = row < a.m;
-  const float* d = a.diag_in + int64_t(t.z) * small;
   float f[16];
-  if (MODE == GRAM) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) f[i] = __uint_as_float(v[i]) * a.descale;
-  } else {
-    const float dr = MODE == APPLY && TALL ? 0.f : in ? d[row] : 0.f;
-    float dc[16];
-    if (MODE == POLY || TALL) {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) dc[i] = col + i < small ? __ldg(d + col + i) : 0.f;
-    }
+  for (int i = 0; i < 16; ++i) f[i] = __uint_as_float(v[i]) * a.gain;
+  if (MODE == APPLY && !TALL) {
+    const float w = kA + p.dr;
 #pragma unroll
     for (int i = 0; i < 16; i += 2) {
       const float2 x = floats_of(b.hi[i >> 1], b.lo[i >> 1]);
-      const float x0 = x.x * a.in_unscale, x1 = x.y * a.in_unscale;
-      const float s0 = __uint_as_float(v[i]) * a.descale, s1 = __uint_as_float(v[i + 1]) * a.descale;
-      if (MODE == APPLY) {
-        f[i] = fmaf(kA + (TALL ? dc[i] : dr), x0, s0);
-        f[i + 1] = fmaf(kA + (TALL ? dc[i + 1] : dr), x1, s1);
-      } else {
-        f[i] = fmaf(kB, x0, kC * fmaf(dr + dc[i], x0, s0));
-        f[i + 1] = fmaf(kB, x1, kC * fmaf(dr + dc[i + 1], x1, s1));
-      }
+      f[i] = fmaf(w, x.x, f[i]);
+      f[i + 1] = fmaf(w, x.y, f[i + 1]);
+    }
+  } else if (MODE != GRAM) {
+    const float w = MODE == POLY ? fmaf(kC, p.dr, kB) : kA, by = MODE == POLY ? kC : 1.f;
+#pragma unroll
+    for (int i = 0; i < 16; i += 2) {
+      const float2 x = floats_of(b.hi[i >> 1], b.lo[i >> 1]);
+      const float d0 = col + i < a.n ? __ldg(p.d + col + i) : 0.f, d1 = col + i + 1 < a.n ? __ldg(p.d + col + i + 1) : 0.f;
+      f[i] = fmaf(fmaf(by, d0, w), x.x, f[i]);
+      f[i + 1] = fmaf(fmaf(by, d1, w), x.y, f[i + 1]);
     }
   }
-  if (MODE != APPLY && !t.turned && in && row - col >= 0 && row - col < 16) {      // the diagonal, kept apart
+  if (MODE != APPLY && p.diag) {                         // the diagonal, kept apart
+    const int at = p.row - col;
     float s = 0.f;
 #pragma unroll
     for (int i = 0; i < 16; ++i)
-      if (col + i == row) { s = MODE == GRAM ? f[i] : __uint_as_float(v[i]) * a.descale; f[i] = 0.f; }
-    if (MODE == POLY) { const float di = d[row]; s = fmaf(kB, di, kC * fmaf(di, di, s)); }
-    a.diag_out[int64_t(t.z) * small + row] = s;
+      if (i == at) { s = __uint_as_float(v[i]) * a.descale; f[i] = 0.f; }
+    if (MODE == POLY) s = fmaf(kB, p.dr, kC * fmaf(p.dr, p.dr, s));
+    if (p.in && at >= 0 && at < 16) a.diag_out[int64_t(t.z) * a.m + p.row] = s;
   }
   if (MODE == APPLY && a.user) {
     typedef typename std::conditional<NPROD == 1, bf16, float>::type T;
-    if (in) store_user(static_cast<T*>(a.user) + t.z * a.user_batch + row * a.user_ld + col, f, a.n - col);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) f[i] *= a.unscale;
+    if (p.in) store_user(static_cast<T*>(a.user) + t.z * a.user_batch + p.row * a.user_ld + col, f, a.n - col);
     return;
   }
-  const bool lo_too = MODE != POLY || NPROD > 1;
+  constexpr bool LO = MODE != POLY || NPROD > 1;
   uint32_t hi[8], lo[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) split2(f[2 * i] * a.out_scale, f[2 * i + 1] * a.out_scale, hi[i], lo[i]);
-  const int64_t base = int64_t(t.z) * a.m * a.ld_out;
-  if (in) {
-    store16(a.out.hi + base + row * a.ld_out + col, hi);
-    if (lo_too) store16(a.out.lo + base + row * a.ld_out + col, lo);
+  for (int i = 0; i < 8; ++i) split2(f[2 * i], f[2 * i + 1], hi[i], lo[i]);
+  if (p.in) {
+    store16(a.out.hi + p.out_at + c, hi);
+    if (LO) store16(a.out.lo + p.out_at + c, lo);
   }
   if (MODE != APPLY && t.turned) {                       // below the diagonal: lane l has half of column l / 2
     __syncwarp();
@@ -378,28 +393,33 @@ __device__ __forceinline__ void finish(const NsArgs& a, const Tile& t, int row, 
       turn[(2 * i + 1) * kTurnPitch + lane] = __byte_perm(hi[i], lo[i], 0x7632);
     }
     __syncwarp();
-    const int c = lane >> 1, row0 = row - lane + (lane & 1) * 16;
-    const uint4* p = reinterpret_cast<const uint4*>(turn + c * kTurnPitch + (lane & 1) * 16);
+    const uint4* from = reinterpret_cast<const uint4*>(turn + (lane >> 1) * kTurnPitch + (lane & 1) * 16);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const uint4 w = p[i];
+      const uint4 w = from[i];
       hi[2 * i] = __byte_perm(w.x, w.y, 0x5410);
       hi[2 * i + 1] = __byte_perm(w.z, w.w, 0x5410);
       lo[2 * i] = __byte_perm(w.x, w.y, 0x7632);
       lo[2 * i + 1] = __byte_perm(w.z, w.w, 0x7632);
     }
-    if (col + c < a.n && row0 < a.ld_out) {              // (beyond m: into the padding)
-      store16(a.out.hi + base + (col + c) * a.ld_out + row0, hi);
-      if (lo_too) store16(a.out.lo + base + (col + c) * a.ld_out + row0, lo);
+    // (rows beyond m: into the padding)
+    if (col + (lane >> 1) < a.n && p.row - lane + (lane & 1) * 16 < a.ld_out) {
+      const int64_t to = p.turn_at + c * a.ld_out;
+      store16(a.out.hi + to, hi);
+      if (LO) store16(a.out.lo + to, lo);
     }
   }
 }
 
+__device__ __forceinline__ void prefetch_map(const CUtensorMap* m) {
+  asm volatile("prefetch.tensormap [%0];" ::"l"(m) : "memory");
+}
+
 struct Maps { CUtensorMap a_hi, a_lo, b_hi, b_lo; };
 
-template <int CTAS, int MODE, bool TALL, int NPROD>
+template <int CTAS, int COLS, int MODE, bool TALL, int NPROD>
 __global__ void __launch_bounds__(kThreads, 1) k_ns_product(const __grid_constant__ Maps maps, const NsArgs a) {
-  using C = Cfg<CTAS, NPROD>;
+  using C = Cfg<CTAS, COLS, NPROD>;
   constexpr bool SYM = MODE != APPLY, A_MN = MODE == GRAM && TALL, B_MN = A_MN || (MODE == APPLY && !TALL);
   extern __shared__ __align__(1024) uint8_t smem[];
   const uint32_t base = smem_u32(smem);
@@ -411,6 +431,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_ns_product(const __grid_constan
   auto bar_acc_full = [&](int b) { return base + C::OFF_BAR + 8u * (2 * C::STAGES + b); };
   auto bar_acc_empty = [&](int b) { return base + C::OFF_BAR + 8u * (2 * C::STAGES + 2 + b); };
   if (threadIdx.x == 0) {
+    prefetch_map(&maps.a_hi);
+    prefetch_map(&maps.b_hi);
+    if (NPROD > 1) { prefetch_map(&maps.a_lo); prefetch_map(&maps.b_lo); }
     for (int s = 0; s < C::STAGES; ++s) { mbar_init(bar_full(s), 1); mbar_init(bar_empty(s), 1); }
     for (int b = 0; b < 2; ++b) { mbar_init(bar_acc_full(b), 1); mbar_init(bar_acc_empty(b), CTAS * kEpiWarps); }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -506,17 +529,18 @@ __global__ void __launch_bounds__(kThreads, 1) k_ns_product(const __grid_constan
       if (!ok) raise(a.status, XRL_ERR_TIMEOUT);
     }
   } else {
-    constexpr int COLS = C::N / 2;       // of a warp
-    const int q = warp & 3, half = (warp - 2) >> 2;
+    constexpr int WC = C::WARP_COLS;
+    const int q = warp & 3, side = (warp - 2) >> 2;
     uint32_t* turn = reinterpret_cast<uint32_t*>(smem + C::OFF_TURN + (warp - 2) * C::TURN_BYTES);
     uint32_t lt = 0;
     bool ok = true;
     for (int tile = first; ok && tile < total; tile += step) {
       const Tile t = tile_of<C::M, C::N, SYM>(a, tile);
-      const int row = t.row + rank * kRows + q * 32 + lane, col = t.col + half * COLS;
-      Beside next;
-      ask<MODE>(a, t.z, row, col, next);
-      float sum[NPROD == 1 ? 1 : COLS];
+      const int row = t.row + rank * kRows + q * 32 + lane, col = t.col + side * WC;
+      const Piece p = piece_of<MODE, TALL>(a, t, row, col, lane);
+      Beside beside;
+      ask<MODE>(a, p, col, 0, beside);
+      float sum[NPROD == 1 ? 1 : WC];
       for (int k0 = 0; k0 < ksteps; ++lt) {
         const int k1 = k0 < ksteps - C::CHUNK ? k0 + C::CHUNK : ksteps, buf = lt & 1;
         uint32_t got = 1;
@@ -528,11 +552,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_ns_product(const __grid_constan
         ok = __shfl_sync(0xFFFFFFFFu, got, 0) != 0;
         if (!ok) break;
         tc_fence_after();
-        const uint32_t taddr = tmem_base + (uint32_t(q * 32) << 16) + uint32_t(buf * C::N + half * COLS);
+        const uint32_t taddr = tmem_base + (uint32_t(q * 32) << 16) + uint32_t(buf * C::N + side * WC);
         if (NPROD > 1 && ksteps > C::CHUNK) {
           // the sums so far; with the last accumulator they go back into its place
 #pragma unroll
-          for (int c = 0; c < COLS; c += 16) {
+          for (int c = 0; c < WC; c += 16) {
             uint32_t v[16];
             tc_ld16(taddr + c, v);
             tc_wait_ld();
@@ -544,20 +568,19 @@ __global__ void __launch_bounds__(kThreads, 1) k_ns_product(const __grid_constan
           }
           if (k1 == ksteps) {
 #pragma unroll
-            for (int c = 0; c < COLS; c += 16) tc_st16(taddr + c, sum + (NPROD == 1 ? 0 : c));
+            for (int c = 0; c < WC; c += 16) tc_st16(taddr + c, sum + (NPROD == 1 ? 0 : c));
             asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
           }
         }
         if (k1 == ksteps) {
 #pragma unroll 1
-          for (int c = 0; c < COLS; c += 16) {
-            const Beside beside = next;
-            if (c + 16 < COLS) ask<MODE>(a, t.z, row, col + c + 16, next);
+          for (int c = 0; c < WC; c += 16) {
+            if (c) ask<MODE>(a, p, col, c, beside);
             __syncwarp();
             uint32_t v[16];
             tc_ld16(taddr + c, v);
             tc_wait_ld();
-            finish<MODE, TALL, NPROD>(a, t, row, col + c, lane, v, beside, turn);
+            finish<MODE, TALL, NPROD>(a, t, p, col, c, lane, v, beside, turn);
           }
         }
         tc_fence_before();
@@ -592,17 +615,19 @@ bool make_map3(CUtensorMap* m, const void* ptr, int batch, int rows, int cols, i
             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
+// fp16 operands as matrices of the workspace
+struct Operand { Half2 p; int rows, cols; int64_t ld; };
 // one operand's pair of maps: its outer index along the rows (K-major, `outer` of them a load) or along the columns (MN-major)
-bool make_operand(CUtensorMap* hi, CUtensorMap* lo, const Half2& p, int batch, int rows, int cols, int64_t ld, bool mn, int outer) {
+bool make_operand(CUtensorMap* hi, CUtensorMap* lo, const Operand& o, int batch, bool mn, int outer, bool both) {
   const uint32_t box = mn ? kStep : outer;
-  return make_map3(hi, p.hi, batch, rows, cols, ld, box) && make_map3(lo, p.lo, batch, rows, cols, ld, box);
+  return make_map3(hi, o.p.hi, batch, o.rows, o.cols, o.ld, box) && (!both || make_map3(lo, o.p.lo, batch, o.rows, o.cols, o.ld, box));
 }
 
-template <int CTAS, int MODE, bool TALL, int NPROD>
-bool launch_product(const Maps& maps, NsArgs a, int batch, cudaStream_t st) {
-  using C = Cfg<CTAS, NPROD>;
+template <int CTAS, int COLS, int MODE, bool TALL, int NPROD>
+bool launch_tiles(const Maps& maps, NsArgs a, int batch, cudaStream_t st) {
+  using C = Cfg<CTAS, COLS, NPROD>;
   static bool done[64] = {};
-  if (!ensure_dynamic_smem(k_ns_product<CTAS, MODE, TALL, NPROD>, C::SMEM_BYTES, done)) return false;
+  if (!ensure_dynamic_smem(k_ns_product<CTAS, COLS, MODE, TALL, NPROD>, C::SMEM_BYTES, done)) return false;
   const int tm = (a.m + C::M - 1) / C::M;
   a.tiles_n = (a.n + C::N - 1) / C::N;
   a.tiles = MODE == APPLY ? tm * a.tiles_n : tm * (tm + 1) / 2 * C::SUB;
@@ -621,7 +646,27 @@ bool launch_product(const Maps& maps, NsArgs a, int batch, cudaStream_t st) {
   at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
   cfg.attrs = at;
   cfg.numAttrs = CTAS > 1 ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, k_ns_product<CTAS, MODE, TALL, NPROD>, maps, a) == cudaSuccess;
+  return cudaLaunchKernelEx(&cfg, k_ns_product<CTAS, COLS, MODE, TALL, NPROD>, maps, a) == cudaSuccess;
+}
+
+// Tiles of a product: of 256 rows by a pair of CTAs where those keep most SMs busy, else of 128 x 128, else of 128 x 64
+template <int MODE, bool TALL, int NPROD>
+bool launch_product(const Operand& left, const Operand& right, const NsArgs& a, int batch, cudaStream_t st) {
+  constexpr bool A_MN = MODE == GRAM && TALL, B_MN = A_MN || (MODE == APPLY && !TALL);
+  constexpr int WIDE = NPROD == 1 ? 256 : 128;           // columns of a pair's tile
+  auto tiles = [&](int m, int n) {
+    const int64_t tm = (a.m + m - 1) / m, tn = (a.n + n - 1) / n;
+    return (MODE == APPLY ? tm * tn : tm * (tm + 1) / 2 * (m / n)) * batch;
+  };
+  const int kind = tiles(256, WIDE) >= 60 ? 2 : tiles(128, 128) >= 100 ? 1 : 0;
+  const int outer = kind == 2 ? WIDE / 2 : kind == 1 ? 128 : 64;
+  Maps maps;
+  if (!make_operand(&maps.a_hi, &maps.a_lo, left, batch, A_MN, kRows, NPROD > 1) ||
+      !make_operand(&maps.b_hi, &maps.b_lo, right, batch, B_MN, outer, NPROD > 1))
+    return false;
+  if (kind == 2) return launch_tiles<2, WIDE, MODE, TALL, NPROD>(maps, a, batch, st);
+  if (kind == 1) return launch_tiles<1, 128, MODE, TALL, NPROD>(maps, a, batch, st);
+  return launch_tiles<1, 64, MODE, TALL, NPROD>(maps, a, batch, st);
 }
 
 // the workspace's pieces
@@ -661,10 +706,9 @@ NsSpace layout(void* ws, int batch, int rows, int cols) {
   return s;
 }
 
-template <typename T, int NPROD, bool TALL, int CTAS>
+template <typename T, int NPROD, bool TALL>
 bool run_steps(int batch, int rows, int cols, const void* grad, int64_t ld, int64_t bs, int steps, double eps, void* out,
                int64_t out_ld, int64_t out_bs, const NsSpace& s, int32_t* status, cudaStream_t st) {
-  using C = Cfg<CTAS, NPROD>;
   const int small = TALL ? cols : rows, large = TALL ? rows : cols;
   int k = int(lround(0.5 * log2(double(rows) * double(cols))));
   if (k > 14) k = 14;
@@ -675,64 +719,46 @@ bool run_steps(int batch, int rows, int cols, const void* grad, int64_t ld, int6
   launch(k_ns_start<T>, dim3(sb, batch), 256, 0, st, static_cast<const T*>(grad), ld, bs, rows, cols, s.partial, nb, eps, xs,
          s.x[0], s.ldx);
 
-  NsArgs sym = {};
-  sym.m = sym.n = small;
-  sym.ld_in = sym.ld_out = s.ldm;
-  sym.out_scale = kGramScale;
-  sym.in_unscale = 1.f / kGramScale;
-  sym.diag_in = s.dA;
-  sym.status = status;
-  NsArgs gram = sym, poly = sym, apply = sym;
+  NsArgs gram = {};
+  gram.m = gram.n = small;
   gram.k = large;
+  gram.ld_in = gram.ld_out = s.ldm;
   gram.descale = 1.f / (xs * xs);
-  gram.out = s.f;
+  gram.gain = kGramScale / (xs * xs);
+  gram.diag_in = s.dA;
   gram.diag_out = s.dA;
+  gram.out = s.f;
+  gram.status = status;
+  NsArgs poly = gram, apply = gram;
   poly.k = small;
   poly.descale = 1.f / (kGramScale * kGramScale);
+  poly.gain = kC / kGramScale;
   poly.in = s.f;
   poly.out = s.b;
   poly.diag_out = s.dB;
   apply.m = rows;
   apply.n = cols;
   apply.k = small;
-  apply.descale = 1.f / (kGramScale * xs);
+  apply.gain = 1.f / kGramScale;
+  apply.unscale = 1.f / xs;
   apply.ld_in = apply.ld_out = s.ldx;
-  apply.in_unscale = 1.f / xs;
-  apply.out_scale = xs;
   apply.diag_in = s.dB;
 
-  Maps mg[2], mp, ma[2];
-  bool ok = make_operand(&mp.a_hi, &mp.a_lo, s.f, batch, small, small, s.ldm, false, kRows) &&
-            make_operand(&mp.b_hi, &mp.b_lo, s.f, batch, small, small, s.ldm, false, C::B_ROWS);
-  for (int i = 0; i < 2; ++i) {
-    ok = ok && make_operand(&mg[i].a_hi, &mg[i].a_lo, s.x[i], batch, rows, cols, s.ldx, TALL, kRows) &&
-         make_operand(&mg[i].b_hi, &mg[i].b_lo, s.x[i], batch, rows, cols, s.ldx, TALL, C::B_ROWS);
-    if (TALL)
-      ok = ok && make_operand(&ma[i].a_hi, &ma[i].a_lo, s.x[i], batch, rows, cols, s.ldx, false, kRows) &&
-           make_operand(&ma[i].b_hi, &ma[i].b_lo, s.b, batch, small, small, s.ldm, false, C::B_ROWS);
-    else
-      ok = ok && make_operand(&ma[i].a_hi, &ma[i].a_lo, s.b, batch, small, small, s.ldm, false, kRows) &&
-           make_operand(&ma[i].b_hi, &ma[i].b_lo, s.x[i], batch, rows, cols, s.ldx, true, C::B_ROWS);
-  }
-  for (int i = 0; ok && i < steps; ++i) {
-    apply.in = s.x[i & 1];
+  const Operand f = {s.f, small, small, s.ldm}, b = {s.b, small, small, s.ldm};
+  for (int i = 0; i < steps; ++i) {
+    const Operand x = {s.x[i & 1], rows, cols, s.ldx};
+    apply.in = x.p;
     apply.out = s.x[(i + 1) & 1];
     if (i == steps - 1) {
       apply.user = out;
       apply.user_ld = out_ld;
       apply.user_batch = out_bs;
     }
-    ok = launch_product<CTAS, GRAM, TALL, NPROD>(mg[i & 1], gram, batch, st) &&
-         launch_product<CTAS, POLY, false, NPROD>(mp, poly, batch, st) &&
-         launch_product<CTAS, APPLY, TALL, NPROD>(ma[i & 1], apply, batch, st);
+    if (!launch_product<GRAM, TALL, NPROD>(x, x, gram, batch, st) || !launch_product<POLY, false, NPROD>(f, f, poly, batch, st) ||
+        !launch_product<APPLY, TALL, NPROD>(TALL ? x : b, TALL ? b : x, apply, batch, st))
+      return false;
   }
-  return ok;
-}
-
-// Pairs of CTAs where their tiles of the square product keep most SMs busy
-bool pairs(int batch, int rows, int cols, int columns) {
-  const int64_t tiles = (int64_t(rows) + 255) / 256 * ((int64_t(cols) + columns - 1) / columns) * batch;
-  return tiles >= 60;
+  return true;
 }
 
 }  // namespace
@@ -744,12 +770,8 @@ bool launch_orthogonalise(int dtype, int32_t batch, int32_t rows, int32_t cols, 
                           int32_t* status, cudaStream_t st) {
   const NsSpace s = layout(workspace, batch, rows, cols);
   if (!status) status = s.status;
-  const bool bf = dtype == XRL_BF16, tall = rows > cols;
-  auto f = pairs(batch, rows, cols, bf ? 256 : 128)
-               ? (bf ? (tall ? run_steps<bf16, 1, true, 2> : run_steps<bf16, 1, false, 2>)
-                     : (tall ? run_steps<float, 3, true, 2> : run_steps<float, 3, false, 2>))
-               : (bf ? (tall ? run_steps<bf16, 1, true, 1> : run_steps<bf16, 1, false, 1>)
-                     : (tall ? run_steps<float, 3, true, 1> : run_steps<float, 3, false, 1>));
+  auto f = dtype == XRL_BF16 ? (rows > cols ? run_steps<bf16, 1, true> : run_steps<bf16, 1, false>)
+                             : (rows > cols ? run_steps<float, 3, true> : run_steps<float, 3, false>);
   return f(batch, rows, cols, grad, ld, batch_stride, steps, double(eps), out, out_ld, out_batch_stride, s, status, st);
 }
 
