@@ -214,6 +214,15 @@ template <int CTAS> __device__ __forceinline__ void arrive_first(uint32_t bar) {
         "mbarrier.arrive.release.cluster.shared::cluster.b64 _, [a];\n\t}" ::"r"(bar) : "memory");
   }
 }
+__device__ __forceinline__ bool elected() {              // true in one lane of a converged warp
+  uint32_t one;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(one));
+  return one != 0;
+}
+// the whole warp, with one answer
+__device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity) {
+  return __all_sync(0xFFFFFFFFu, mbar_wait(bar, parity));
+}
 template <int CTAS> __device__ __forceinline__ void tile_sync() {      // all threads of the CTA, of a pair of both
   if (CTAS == 1) __syncthreads();
   else asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
@@ -423,7 +432,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_ns_product(const __grid_constan
   constexpr bool SYM = MODE != APPLY, A_MN = MODE == GRAM && TALL, B_MN = A_MN || (MODE == APPLY && !TALL);
   extern __shared__ __align__(1024) uint8_t smem[];
   const uint32_t base = smem_u32(smem);
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = __shfl_sync(0xFFFFFFFFu, int(threadIdx.x) >> 5, 0), lane = threadIdx.x & 31;
   const int rank = int(blockIdx.x) % CTAS, first = int(blockIdx.x) / CTAS, step = int(gridDim.x) / CTAS;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + C::OFF_TMEM);
   auto bar_full = [&](int s) { return base + C::OFF_BAR + 8u * s; };
@@ -454,7 +463,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_ns_product(const __grid_constan
   __syncwarp();
   tile_sync<CTAS>();
   tc_fence_after();
-  const uint32_t tmem_base = *tmem_slot;
+  const uint32_t tmem_base = __shfl_sync(0xFFFFFFFFu, *tmem_slot, 0);
   int total = a.total;
   if ((base & 1023u) != 0) {             // the swizzle's pattern starts on 1,024 bytes
     total = 0;
@@ -463,20 +472,23 @@ __global__ void __launch_bounds__(kThreads, 1) k_ns_product(const __grid_constan
   const int ksteps = (a.k + kStep - 1) / kStep;
   enter();
 
+  // Both of the next roles run with the whole warp, one lane of which issues: what the loops carry is then the same for all
+  // lanes and stays in uniform registers, where the instructions want it.  (Run by one lane alone, a product instruction cost
+  // that lane some 115 cycles, and a 256 x 256 x 16 product takes 128: 4,096 square bf16 1,504 us.)
   if (warp == 0) {
-    if (lane == 0) {
-      uint32_t it = 0;
-      bool ok = true;
-      fence_async_all();
-      for (int tile = first; ok && tile < total; tile += step) {
-        const Tile t = tile_of<C::M, C::N, SYM>(a, tile);
-        const int row = t.row + rank * kRows, col = t.col + rank * C::B_ROWS;
-        for (int k = 0; k < ksteps; ++k, ++it) {
-          const int s = it % C::STAGES;
-          const uint32_t round = it / C::STAGES;
-          if (round > 0 && !mbar_wait(bar_empty(s), (round - 1) & 1)) { ok = false; break; }
+    uint32_t it = 0;
+    bool ok = true;
+    fence_async_all();
+    for (int tile = first; ok && tile < total; tile += step) {
+      const Tile t = tile_of<C::M, C::N, SYM>(a, tile);
+      const int row = t.row + rank * kRows, col = t.col + rank * C::B_ROWS;
+      for (int k = 0; k < ksteps; ++k, ++it) {
+        const int s = it % C::STAGES;
+        const uint32_t round = it / C::STAGES;
+        if (round > 0 && !wait_warp(bar_empty(s), (round - 1) & 1)) { ok = false; break; }
+        const uint32_t at = base + s * C::STAGE;
+        if (elected()) {
           if (rank == 0) mbar_expect_tx(bar_full(s), CTAS * C::STAGE);
-          const uint32_t at = base + s * C::STAGE;
           load_operand<CTAS, A_MN, kRows>(at, &maps.a_hi, row, k * kStep, t.z, bar_full(s));
           load_operand<CTAS, B_MN, C::B_ROWS>(at + C::OFF_B, &maps.b_hi, col, k * kStep, t.z, bar_full(s));
           if (NPROD > 1) {
@@ -484,49 +496,54 @@ __global__ void __launch_bounds__(kThreads, 1) k_ns_product(const __grid_constan
             load_operand<CTAS, B_MN, C::B_ROWS>(at + C::OFF_B + C::B_BYTES, &maps.b_lo, col, k * kStep, t.z, bar_full(s));
           }
         }
-      }
-      if (!ok) {                         // the copies in flight land within microseconds of a wait that took seconds
-        raise(a.status, XRL_ERR_TIMEOUT);
-        const unsigned long long t0 = now_ns();
-        while (now_ns() - t0 < 5000000ull) {}
+        __syncwarp();
       }
     }
+    if (!ok) {                           // the copies in flight land within microseconds of a wait that took seconds
+      if (lane == 0) raise(a.status, XRL_ERR_TIMEOUT);
+      const unsigned long long t0 = now_ns();
+      while (now_ns() - t0 < 5000000ull) {}
+    }
   } else if (warp == 1) {
-    if (lane == 0 && rank == 0) {
+    if (rank == 0) {
       // fp32 accumulators, fp16 x fp16; bits 15 and 16: MN-major operands
       constexpr uint32_t idesc = (1u << 4) | (A_MN ? 1u << 15 : 0u) | (B_MN ? 1u << 16 : 0u) | (uint32_t(C::N >> 3) << 17) |
                                  (uint32_t(C::M >> 4) << 24);
+      // a descriptor's address counts 16 bytes from its lowest bit
+      const uint64_t a0 = operand_desc<A_MN>(base, 0), b0 = operand_desc<B_MN>(base + C::OFF_B, 0);
+      constexpr int A_K = (A_MN ? 2048 : 32) >> 4, B_K = (B_MN ? 2048 : 32) >> 4, A_LO = C::A_BYTES >> 4, B_LO = C::B_BYTES >> 4;
       uint32_t it = 0, lt = 0;
       bool ok = true;
       for (int tile = first; ok && tile < total; tile += step) {
         for (int k0 = 0; ok && k0 < ksteps; k0 = k0 < ksteps - C::CHUNK ? k0 + C::CHUNK : ksteps, ++lt) {
           const int k1 = k0 < ksteps - C::CHUNK ? k0 + C::CHUNK : ksteps, buf = lt & 1;
-          if (lt > 1 && !mbar_wait(bar_acc_empty(buf), ((lt >> 1) - 1) & 1)) { ok = false; break; }
+          if (lt > 1 && !wait_warp(bar_acc_empty(buf), ((lt >> 1) - 1) & 1)) { ok = false; break; }
           tc_fence_after();
           const uint32_t acc = tmem_base + uint32_t(buf * C::N);
           for (int k = k0; k < k1; ++k, ++it) {
             const int s = it % C::STAGES;
-            if (!mbar_wait(bar_full(s), (it / C::STAGES) & 1)) { ok = false; break; }
+            if (!wait_warp(bar_full(s), (it / C::STAGES) & 1)) { ok = false; break; }
             tc_fence_after();
-            const uint32_t at = base + s * C::STAGE;
-            if (NPROD > 1) {
+            const uint64_t da = a0 + uint64_t(s * (C::STAGE >> 4)), db = b0 + uint64_t(s * (C::STAGE >> 4));
+            if (elected()) {
+              if (NPROD > 1) {
 #pragma unroll
-              for (int kk = 0; kk < kStep / 16; ++kk) {
-                mma<CTAS>(acc, operand_desc<A_MN>(at, kk), operand_desc<B_MN>(at + C::OFF_B + C::B_BYTES, kk), idesc,
-                          k > k0 || kk ? 1u : 0u);
-                mma<CTAS>(acc, operand_desc<A_MN>(at + C::A_BYTES, kk), operand_desc<B_MN>(at + C::OFF_B, kk), idesc, 1u);
+                for (int kk = 0; kk < kStep / 16; ++kk) {
+                  mma<CTAS>(acc, da + kk * A_K, db + kk * B_K + B_LO, idesc, k > k0 || kk ? 1u : 0u);
+                  mma<CTAS>(acc, da + kk * A_K + A_LO, db + kk * B_K, idesc, 1u);
+                }
               }
-            }
 #pragma unroll
-            for (int kk = 0; kk < kStep / 16; ++kk)
-              mma<CTAS>(acc, operand_desc<A_MN>(at, kk), operand_desc<B_MN>(at + C::OFF_B, kk), idesc,
-                        NPROD > 1 || k > k0 || kk ? 1u : 0u);
-            commit<CTAS>(bar_empty(s));
+              for (int kk = 0; kk < kStep / 16; ++kk)
+                mma<CTAS>(acc, da + kk * A_K, db + kk * B_K, idesc, NPROD > 1 || k > k0 || kk ? 1u : 0u);
+              commit<CTAS>(bar_empty(s));
+              if (k + 1 == k1) commit<CTAS>(bar_acc_full(buf));
+            }
+            __syncwarp();
           }
-          if (ok) commit<CTAS>(bar_acc_full(buf));
         }
       }
-      if (!ok) raise(a.status, XRL_ERR_TIMEOUT);
+      if (!ok && lane == 0) raise(a.status, XRL_ERR_TIMEOUT);
     }
   } else {
     constexpr int WC = C::WARP_COLS;
