@@ -129,13 +129,10 @@ struct NsArgs {
   int total;                             // tiles of all matrices
   float descale;                         // accumulator -> value
   float gain;                            // accumulator -> its share of the scaled result
-  Half2 in;                              // POLY: F; APPLY: X (the product's shape and the result's scale)
-  int64_t ld_in;
-  const float* diag_in;                  // [batch x small side]
-  Half2 out;
-  int64_t ld_out;
+  const float* diag_in;                  // [batch][diag_stride]
   float* diag_out;
-  void* user;                            // APPLY: the caller's matrices in place of `out`
+  int64_t diag_stride;
+  void* user;                            // APPLY: the caller's matrices in place of the next X
   int64_t user_ld, user_batch;
   float unscale;                         // scaled result -> the caller's
   int32_t* status;
@@ -143,7 +140,7 @@ struct NsArgs {
 
 constexpr int kRows = 128, kStep = 64;   // rows of the result per CTA, reduction per stage
 constexpr int kEpiWarps = 16, kThreads = 64 + 32 * kEpiWarps;
-constexpr int kTurnPitch = 36;           // words per column of a warp's 32 x 16 piece that is being transposed
+constexpr int kBlockBytes = 32 * 32 * 2; // a 32 x 32 piece of an epilogue warp: rows of 64 bytes, 64-byte swizzle
 
 // CTAS: of a tile.  A pair multiplies 256 rows by N columns with one instruction; each holds its 128 rows of the left operand
 // and N / 2 of the right one, so a tile of 256 x 256 asks half of what four of 128 x 128 do of L2.
@@ -160,15 +157,17 @@ template <int CTAS, int COLS, int NPROD> struct Cfg {
   static constexpr int PARTS = NPROD == 1 ? 1 : 2;        // hi; hi and lo
   static constexpr int OFF_B = PARTS * A_BYTES;           // a stage: A hi, A lo, B hi, B lo
   static constexpr int STAGE = PARTS * (A_BYTES + B_BYTES);
-  static constexpr int STAGES = 184 * 1024 / STAGE < 6 ? 184 * 1024 / STAGE : 6;
-  static constexpr int OFF_TURN = STAGES * STAGE;
-  static constexpr int TURN_BYTES = 16 * kTurnPitch * 4;
-  static constexpr int OFF_BAR = OFF_TURN + kEpiWarps * TURN_BYTES;
-  static constexpr int OFF_TMEM = OFF_BAR + 8 * (2 * STAGES + 4);
+  static constexpr int STAGE_BYTES = kEpiWarps * 2 * kBlockBytes;
+  static constexpr int MOST = (227 * 1024 - STAGE_BYTES - 512) / STAGE;
+  static constexpr int STAGES = MOST < 6 ? MOST : 6;
+  static constexpr int OFF_BLOCKS = STAGES * STAGE;       // two pieces per epilogue warp: hi and lo
+  static constexpr int OFF_BAR = OFF_BLOCKS + STAGE_BYTES;
+  static constexpr int OFF_TMEM = OFF_BAR + 8 * (2 * STAGES + 4 + kEpiWarps);
   static constexpr int SMEM_BYTES = OFF_TMEM + 16;
   static constexpr int TMEM_COLS = 2 * N;
-  static constexpr int WARP_COLS = N / (kEpiWarps / 4);   // of an epilogue warp
-  static_assert(SMEM_BYTES <= 227 * 1024 && M % N == 0 && WARP_COLS % 16 == 0, "shared memory of one SM, whole squares");
+  static constexpr int WARP_COLS = N == 256 ? 64 : 32;    // of an epilogue warp
+  static constexpr int WORKERS = 4 * (N / WARP_COLS);     // epilogue warps with something to do
+  static_assert(SMEM_BYTES <= 227 * 1024 && M % N == 0 && WORKERS <= kEpiWarps, "shared memory of one SM, whole squares");
 };
 
 // of a pair, every copy reports to the first CTA's barrier (the same offset; bit 24 of a shared address tells the two apart)
@@ -227,6 +226,11 @@ template <int CTAS> __device__ __forceinline__ void tile_sync() {      // all th
   if (CTAS == 1) __syncthreads();
   else asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
 }
+// After a wait that ran out in seconds: copies in flight take microseconds
+__device__ __forceinline__ void let_copies_land() {
+  const unsigned long long t0 = now_ns();
+  while (now_ns() - t0 < 5000000ull) {}
+}
 // MN-major, 128-byte swizzle: 64 entries of the outer index by 8 of the reduction in 1,024 bytes, 64 x 64 chunks 8 KB apart
 __device__ __forceinline__ uint64_t smem_desc_mn(uint32_t addr) {
   return uint64_t((addr & 0x3FFFFu) >> 4) | (uint64_t(8192 >> 4) << 16) | (uint64_t(1024 >> 4) << 32) | (uint64_t(1) << 46) |
@@ -284,147 +288,205 @@ __device__ __forceinline__ void tc_st16(uint32_t taddr, const float* r) {
       ::"r"(u[0]), "r"(u[1]), "r"(u[2]), "r"(u[3]), "r"(u[4]), "r"(u[5]), "r"(u[6]), "r"(u[7]), "r"(u[8]), "r"(u[9]),
         "r"(u[10]), "r"(u[11]), "r"(u[12]), "r"(u[13]), "r"(u[14]), "r"(u[15]), "r"(taddr) : "memory");
 }
-// 16 fp16 numbers
-__device__ __forceinline__ void load16(const __half* p, uint32_t (&r)[8]) {
-  const uint4 a = *reinterpret_cast<const uint4*>(p), b = *reinterpret_cast<const uint4*>(p + 8);
-  r[0] = a.x; r[1] = a.y; r[2] = a.z; r[3] = a.w;
-  r[4] = b.x; r[5] = b.y; r[6] = b.z; r[7] = b.w;
+// 16 rows by 32 columns: lane l has columns 8 c + 2 (l % 4) and the next one, of row l / 4 in r[4 c], r[4 c + 1] and of row
+// l / 4 + 8 in the two after them - which is how ldmatrix and stmatrix hand out 8 x 8 blocks of 16-bit numbers
+__device__ __forceinline__ void tc_ld_blocks(uint32_t taddr, uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.16x256b.x4.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+        "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]) : "r"(taddr) : "memory");
 }
-__device__ __forceinline__ void store16(__half* p, const uint32_t (&r)[8]) {
-  store32(p, r[0], r[1], r[2], r[3], r[4], r[5], r[6], r[7]);
+__device__ __forceinline__ void ldmatrix4(uint32_t at, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
+}
+template <bool TURN> __device__ __forceinline__ void stmatrix4(uint32_t at, const uint32_t* r) {
+  if (TURN)
+    asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};"
+                 ::"r"(at), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]) : "memory");
+  else
+    asm volatile("stmatrix.sync.aligned.m8n8.x4.shared.b16 [%0], {%1, %2, %3, %4};"
+                 ::"r"(at), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]) : "memory");
+}
+__device__ __forceinline__ void tma_store_3d(const CUtensorMap* map, uint32_t src, int x, int y, int z) {
+  asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%2, %3, %4}], [%1];"
+               ::"l"(map), "r"(src), "r"(x), "r"(y), "r"(z) : "memory");
 }
 __device__ __forceinline__ float2 floats_of(uint32_t hi, uint32_t lo) {
   const float2 h = __half22float2(*reinterpret_cast<const __half2*>(&hi)), l = __half22float2(*reinterpret_cast<const __half2*>(&lo));
   return make_float2(h.x + l.x, h.y + l.y);
 }
-template <typename T> __device__ __forceinline__ void store_user(T* p, const float (&v)[16], int count) {
-  constexpr int N = VecOf<T>::N;
-  if (count >= 16 && (reinterpret_cast<uintptr_t>(p) & 15) == 0) {
-#pragma unroll
-    for (int i = 0; i < 16; i += N) {
-      float f[N];
-#pragma unroll
-      for (int t = 0; t < N; ++t) f[t] = v[i + t];
-      store_vec(p + i, f);
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 16; ++i)
-      if (i < count) p[i] = T(v[i]);
-  }
+// 16 bytes `chunk` of row `row` of a piece
+__device__ __forceinline__ uint32_t block_at(uint32_t piece, int row, int chunk) {
+  return piece + row * 64 + ((chunk ^ ((row >> 1) & 3)) << 4);
 }
 
-// An epilogue warp's part of a tile: 32 rows, a lane each, by 16 columns at a time
-struct Piece {
-  bool in, diag;                         // the row is the matrix's; the warp's part can hold diagonal entries
-  int row;
-  int64_t in_at, out_at, turn_at;        // of the lane's row in `in` and `out`; of its half column below the diagonal
-  const float* d;                        // diagonal of the matrix
-  float dr;                              // the row's own
+struct Maps { CUtensorMap a_hi, a_lo, b_hi, b_lo, in_hi, in_lo, out_hi, out_lo; };
+
+// An epilogue warp's pieces of 32 x 32.  What a piece reads besides the accumulator (`in`: F or X) comes by TMA to where its
+// result will be; the result goes through shared memory to the TMA unit, and its transpose after it.
+struct Pieces {
+  uint32_t hi, bar;                      // lo: kBlockBytes behind hi
+  uint32_t phase = 0;
+  int lane;
 };
-template <int MODE, bool TALL>
-__device__ __forceinline__ Piece piece_of(const NsArgs& a, const Tile& t, int row, int col, int lane) {
-  Piece p;
-  p.row = row;
-  p.in = row < a.m;
-  p.diag = MODE != APPLY && !t.turned && row - lane < col + 256 && col < row - lane + 32;
-  const int64_t r = int64_t(t.z) * a.m + row;
-  p.in_at = r * a.ld_in + col;
-  p.out_at = r * a.ld_out + col;
-  p.turn_at = (int64_t(t.z) * a.m + col + (lane >> 1)) * a.ld_out + (row - lane + (lane & 1) * 16);
-  p.d = a.diag_in + int64_t(t.z) * (TALL ? a.n : a.m);
-  p.dr = MODE == GRAM || (MODE == APPLY && TALL) || !p.in ? 0.f : p.d[row];
-  return p;
-}
-struct Beside { uint32_t hi[8], lo[8]; };                // 16 entries of `in`
 template <int MODE>
-__device__ __forceinline__ void ask(const NsArgs& a, const Piece& p, int col, int c, Beside& b) {
-  if (MODE == GRAM || !p.in || col + c >= a.n) return;
-  load16(a.in.hi + p.in_at + c, b.hi);
-  load16(a.in.lo + p.in_at + c, b.lo);
+__device__ __forceinline__ void ask(const Maps& maps, const NsArgs& a, Pieces& w, int z, int row, int col) {
+  if (MODE == GRAM || row >= a.m || col >= a.n) return;
+  fence_async_smem();                    // behind what the warp itself read and wrote here
+  __syncwarp();
+  if (w.lane == 0) {
+    tma_wait_read<0>();                  // the stores that left from here have been read
+    mbar_expect_tx(w.bar, 2 * kBlockBytes);
+    tma_load_3d<1>(w.hi, &maps.in_hi, col, row, z, w.bar);
+    tma_load_3d<1>(w.hi + kBlockBytes, &maps.in_lo, col, row, z, w.bar);
+  }
 }
-// Columns col + c ... + 15 of the next operand from the accumulator's v
 template <int MODE, bool TALL, int NPROD>
-__device__ __forceinline__ void finish(const NsArgs& a, const Tile& t, const Piece& p, int col0, int c, int lane,
-                                       const uint32_t (&v)[16], const Beside& b, uint32_t* turn) {
-  const int col = col0 + c;
-  if (col >= a.n) return;                                // all lanes
-  float f[16];
+__device__ __forceinline__ bool finish(const Maps& maps, const NsArgs& a, Pieces& w, const Tile& t, int row, int col,
+                                       uint32_t taddr) {
+  if (row >= a.m || col >= a.n) return true;             // the whole warp
+  const int lane = w.lane, r = lane >> 2, c = (lane & 3) * 2;
+  const uint32_t lo_piece = w.hi + kBlockBytes;
+  const float* d = a.diag_in + t.z * a.diag_stride;
+  float dr[4];
+  float2 dc[4];
 #pragma unroll
-  for (int i = 0; i < 16; ++i) f[i] = __uint_as_float(v[i]) * a.gain;
-  if (MODE == APPLY && !TALL) {
-    const float w = kA + p.dr;
-#pragma unroll
-    for (int i = 0; i < 16; i += 2) {
-      const float2 x = floats_of(b.hi[i >> 1], b.lo[i >> 1]);
-      f[i] = fmaf(w, x.x, f[i]);
-      f[i + 1] = fmaf(w, x.y, f[i + 1]);
-    }
-  } else if (MODE != GRAM) {
-    const float w = MODE == POLY ? fmaf(kC, p.dr, kB) : kA, by = MODE == POLY ? kC : 1.f;
-#pragma unroll
-    for (int i = 0; i < 16; i += 2) {
-      const float2 x = floats_of(b.hi[i >> 1], b.lo[i >> 1]);
-      const float d0 = col + i < a.n ? __ldg(p.d + col + i) : 0.f, d1 = col + i + 1 < a.n ? __ldg(p.d + col + i + 1) : 0.f;
-      f[i] = fmaf(fmaf(by, d0, w), x.x, f[i]);
-      f[i + 1] = fmaf(fmaf(by, d1, w), x.y, f[i + 1]);
-    }
+  for (int i = 0; i < 4; ++i) {                          // (beyond the matrix: the padding's, for entries that are clipped)
+    dr[i] = MODE == POLY || (MODE == APPLY && !TALL) ? __ldg(d + row + 8 * i + r) : 0.f;
+    dc[i] = MODE == POLY || (MODE == APPLY && TALL) ? __ldg(reinterpret_cast<const float2*>(d + col + 8 * i + c)) : make_float2(0.f, 0.f);
   }
-  if (MODE != APPLY && p.diag) {                         // the diagonal, kept apart
-    const int at = p.row - col;
-    float s = 0.f;
-#pragma unroll
-    for (int i = 0; i < 16; ++i)
-      if (i == at) { s = __uint_as_float(v[i]) * a.descale; f[i] = 0.f; }
-    if (MODE == POLY) s = fmaf(kB, p.dr, kC * fmaf(p.dr, p.dr, s));
-    if (p.in && at >= 0 && at < 16) a.diag_out[int64_t(t.z) * a.m + p.row] = s;
-  }
-  if (MODE == APPLY && a.user) {
-    typedef typename std::conditional<NPROD == 1, bf16, float>::type T;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) f[i] *= a.unscale;
-    if (p.in) store_user(static_cast<T*>(a.user) + t.z * a.user_batch + p.row * a.user_ld + col, f, a.n - col);
-    return;
+  if (MODE != GRAM) {
+    if (!wait_warp(w.bar, w.phase)) return false;
+    w.phase ^= 1;
+  } else {
+    if (lane == 0) tma_wait_read<0>();
+    __syncwarp();
   }
   constexpr bool LO = MODE != POLY || NPROD > 1;
-  uint32_t hi[8], lo[8];
+  const bool user = MODE == APPLY && a.user;
+  uint32_t hi[4][4], lo[4][4];                           // 8 x 8 blocks of the result
 #pragma unroll
-  for (int i = 0; i < 8; ++i) split2(f[2 * i], f[2 * i + 1], hi[i], lo[i]);
-  if (p.in) {
-    store16(a.out.hi + p.out_at + c, hi);
-    if (LO) store16(a.out.lo + p.out_at + c, lo);
+  for (int h = 0; h < 2; ++h) {
+    uint32_t v[16];
+    tc_ld_blocks(taddr + (uint32_t(h * 16) << 16), v);
+    tc_wait_ld();
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      const int rb = 2 * h + s;
+      const uint32_t at = block_at(w.hi, rb * 8 + (lane & 7), lane >> 3);
+      uint32_t xh[4], xl[4];
+      if (MODE != GRAM) {
+        ldmatrix4(at, xh);
+        ldmatrix4(at + kBlockBytes, xl);
+      }
+#pragma unroll
+      for (int cb = 0; cb < 4; ++cb) {
+        const float v0 = __uint_as_float(v[4 * cb + 2 * s]), v1 = __uint_as_float(v[4 * cb + 2 * s + 1]);
+        float f0 = v0 * a.gain, f1 = v1 * a.gain;
+        if (MODE != GRAM) {
+          const float2 x = floats_of(xh[cb], xl[cb]);
+          const float w0 = MODE == POLY ? fmaf(kC, dr[rb] + dc[cb].x, kB) : kA + (TALL ? dc[cb].x : dr[rb]);
+          const float w1 = MODE == POLY ? fmaf(kC, dr[rb] + dc[cb].y, kB) : kA + (TALL ? dc[cb].y : dr[rb]);
+          f0 = fmaf(w0, x.x, f0);
+          f1 = fmaf(w1, x.y, f1);
+        }
+        if (MODE != APPLY && rb == cb && row == col && (r == c || r == c + 1)) {       // the diagonal, kept apart
+          float q = (r == c ? v0 : v1) * a.descale;
+          if (MODE == POLY) q = fmaf(kB, dr[rb], kC * fmaf(dr[rb], dr[rb], q));
+          if (row + 8 * rb + r < a.m) a.diag_out[t.z * a.diag_stride + row + 8 * rb + r] = q;
+          if (r == c) f0 = 0.f;
+          else f1 = 0.f;
+        }
+        if (user) {
+          f0 *= a.unscale;
+          f1 *= a.unscale;
+          if (NPROD == 1) {
+            hi[rb][cb] = pack_bf16x2(f0, f1);
+          } else {                                       // rows of 128 bytes over both pieces, after all of `in` is read
+            hi[rb][cb] = __float_as_uint(f0);
+            lo[rb][cb] = __float_as_uint(f1);
+          }
+        } else {
+          split2(f0, f1, hi[rb][cb], lo[rb][cb]);
+        }
+      }
+      if (!user) {
+        stmatrix4<false>(at, hi[rb]);
+        if (LO) stmatrix4<false>(at + kBlockBytes, lo[rb]);
+      } else if (NPROD == 1) {
+        stmatrix4<false>(at, hi[rb]);
+      }
+    }
   }
-  if (MODE != APPLY && t.turned) {                       // below the diagonal: lane l has half of column l / 2
+  if (user) {
+    typedef typename std::conditional<NPROD == 1, bf16, float>::type T;
+    constexpr int N = VecOf<T>::N, CHUNKS = 32 / N;      // 16-byte chunks of a row
+    __syncwarp();
+    if (NPROD > 1) {
+#pragma unroll
+      for (int rb = 0; rb < 4; ++rb)
+#pragma unroll
+        for (int cb = 0; cb < 4; ++cb) {
+          const int y = rb * 8 + r, chunk = (cb * 8 + c) >> 2;
+          asm volatile("st.shared.v2.b32 [%0], {%1, %2};"
+                       ::"r"(w.hi + y * 128 + ((chunk ^ (y & 7)) << 4) + (c & 2) * 4), "r"(hi[rb][cb]), "r"(lo[rb][cb]) : "memory");
+        }
+      __syncwarp();
+    }
+    T* out = static_cast<T*>(a.user) + t.z * a.user_batch + col;
+#pragma unroll
+    for (int i = 0; i < CHUNKS; ++i) {
+      const int y = (i * 32 + lane) / CHUNKS, chunk = lane % CHUNKS;
+      const uint32_t at = NPROD == 1 ? block_at(w.hi, y, chunk) : w.hi + y * 128 + ((chunk ^ (y & 7)) << 4);
+      uint4 q;
+      asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(q.x), "=r"(q.y), "=r"(q.z), "=r"(q.w) : "r"(at) : "memory");
+      if (row + y < a.m) {
+        T* p = out + (row + y) * a.user_ld + chunk * N;
+        const int left = a.n - col - chunk * N;
+        if (left >= N && (reinterpret_cast<uintptr_t>(p) & 15) == 0) {
+          *reinterpret_cast<uint4*>(p) = q;
+        } else {
+          const T* e = reinterpret_cast<const T*>(&q);
+#pragma unroll
+          for (int j = 0; j < N; ++j)
+            if (j < left) p[j] = e[j];
+        }
+      }
+    }
+    __syncwarp();
+    return true;
+  }
+  fence_async_smem();
+  __syncwarp();
+  if (lane == 0) {
+    tma_store_3d(&maps.out_hi, w.hi, col, row, t.z);
+    if (LO) tma_store_3d(&maps.out_lo, lo_piece, col, row, t.z);
+    tma_commit();
+  }
+  if (MODE != APPLY && t.turned) {                       // below the diagonal
+    if (lane == 0) tma_wait_read<0>();
     __syncwarp();
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      turn[(2 * i) * kTurnPitch + lane] = __byte_perm(hi[i], lo[i], 0x5410);
-      turn[(2 * i + 1) * kTurnPitch + lane] = __byte_perm(hi[i], lo[i], 0x7632);
+    for (int rb = 0; rb < 4; ++rb) {
+      stmatrix4<true>(block_at(w.hi, lane, rb), hi[rb]);
+      if (LO) stmatrix4<true>(block_at(lo_piece, lane, rb), lo[rb]);
     }
+    fence_async_smem();
     __syncwarp();
-    const uint4* from = reinterpret_cast<const uint4*>(turn + (lane >> 1) * kTurnPitch + (lane & 1) * 16);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const uint4 w = from[i];
-      hi[2 * i] = __byte_perm(w.x, w.y, 0x5410);
-      hi[2 * i + 1] = __byte_perm(w.z, w.w, 0x5410);
-      lo[2 * i] = __byte_perm(w.x, w.y, 0x7632);
-      lo[2 * i + 1] = __byte_perm(w.z, w.w, 0x7632);
-    }
-    // (rows beyond m: into the padding)
-    if (col + (lane >> 1) < a.n && p.row - lane + (lane & 1) * 16 < a.ld_out) {
-      const int64_t to = p.turn_at + c * a.ld_out;
-      store16(a.out.hi + to, hi);
-      if (LO) store16(a.out.lo + to, lo);
+    if (lane == 0) {
+      tma_store_3d(&maps.out_hi, w.hi, row, col, t.z);
+      if (LO) tma_store_3d(&maps.out_lo, lo_piece, row, col, t.z);
+      tma_commit();
     }
   }
+  return true;
 }
 
 __device__ __forceinline__ void prefetch_map(const CUtensorMap* m) {
   asm volatile("prefetch.tensormap [%0];" ::"l"(m) : "memory");
 }
-
-struct Maps { CUtensorMap a_hi, a_lo, b_hi, b_lo; };
 
 template <int CTAS, int COLS, int MODE, bool TALL, int NPROD>
 __global__ void __launch_bounds__(kThreads, 1) k_ns_product(const __grid_constant__ Maps maps, const NsArgs a) {
@@ -439,12 +501,15 @@ __global__ void __launch_bounds__(kThreads, 1) k_ns_product(const __grid_constan
   auto bar_empty = [&](int s) { return base + C::OFF_BAR + 8u * (C::STAGES + s); };
   auto bar_acc_full = [&](int b) { return base + C::OFF_BAR + 8u * (2 * C::STAGES + b); };
   auto bar_acc_empty = [&](int b) { return base + C::OFF_BAR + 8u * (2 * C::STAGES + 2 + b); };
+  auto bar_in = [&](int w) { return base + C::OFF_BAR + 8u * (2 * C::STAGES + 4 + w); };
   if (threadIdx.x == 0) {
     prefetch_map(&maps.a_hi);
     prefetch_map(&maps.b_hi);
     if (NPROD > 1) { prefetch_map(&maps.a_lo); prefetch_map(&maps.b_lo); }
+    if (MODE != GRAM) { prefetch_map(&maps.in_hi); prefetch_map(&maps.in_lo); }
+    for (int w = 0; w < kEpiWarps; ++w) mbar_init(bar_in(w), 1);
     for (int s = 0; s < C::STAGES; ++s) { mbar_init(bar_full(s), 1); mbar_init(bar_empty(s), 1); }
-    for (int b = 0; b < 2; ++b) { mbar_init(bar_acc_full(b), 1); mbar_init(bar_acc_empty(b), CTAS * kEpiWarps); }
+    for (int b = 0; b < 2; ++b) { mbar_init(bar_acc_full(b), 1); mbar_init(bar_acc_empty(b), CTAS * C::WORKERS); }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     fence_async_smem();
   }
@@ -499,10 +564,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_ns_product(const __grid_constan
         __syncwarp();
       }
     }
-    if (!ok) {                           // the copies in flight land within microseconds of a wait that took seconds
+    if (!ok) {
       if (lane == 0) raise(a.status, XRL_ERR_TIMEOUT);
-      const unsigned long long t0 = now_ns();
-      while (now_ns() - t0 < 5000000ull) {}
+      let_copies_land();
     }
   } else if (warp == 1) {
     if (rank == 0) {
@@ -545,28 +609,24 @@ __global__ void __launch_bounds__(kThreads, 1) k_ns_product(const __grid_constan
       }
       if (!ok && lane == 0) raise(a.status, XRL_ERR_TIMEOUT);
     }
-  } else {
+  } else if (warp - 2 < C::WORKERS) {
     constexpr int WC = C::WARP_COLS;
     const int q = warp & 3, side = (warp - 2) >> 2;
-    uint32_t* turn = reinterpret_cast<uint32_t*>(smem + C::OFF_TURN + (warp - 2) * C::TURN_BYTES);
+    Pieces w;
+    w.hi = base + C::OFF_BLOCKS + (warp - 2) * 2 * kBlockBytes;
+    w.bar = bar_in(warp - 2);
+    w.lane = lane;
     uint32_t lt = 0;
     bool ok = true;
     for (int tile = first; ok && tile < total; tile += step) {
       const Tile t = tile_of<C::M, C::N, SYM>(a, tile);
-      const int row = t.row + rank * kRows + q * 32 + lane, col = t.col + side * WC;
-      const Piece p = piece_of<MODE, TALL>(a, t, row, col, lane);
-      Beside beside;
-      ask<MODE>(a, p, col, 0, beside);
+      const int row = t.row + rank * kRows + q * 32, col = t.col + side * WC;
+      ask<MODE>(maps, a, w, t.z, row, col);
       float sum[NPROD == 1 ? 1 : WC];
       for (int k0 = 0; k0 < ksteps; ++lt) {
         const int k1 = k0 < ksteps - C::CHUNK ? k0 + C::CHUNK : ksteps, buf = lt & 1;
-        uint32_t got = 1;
-        if (lane == 0) {
-          got = 0;                       // a whole tile is multiplied first: the limit of one wait, several times over
-          for (int w = 0; w < 4 && !got; ++w) got = mbar_wait(bar_acc_full(buf), (lt >> 1) & 1) ? 1u : 0u;
-          if (!got) raise(a.status, XRL_ERR_TIMEOUT);
-        }
-        ok = __shfl_sync(0xFFFFFFFFu, got, 0) != 0;
+        ok = false;                      // a whole tile is multiplied first: the limit of one wait, several times over
+        for (int i = 0; i < 4 && !ok; ++i) ok = wait_warp(bar_acc_full(buf), (lt >> 1) & 1);
         if (!ok) break;
         tc_fence_after();
         const uint32_t taddr = tmem_base + (uint32_t(q * 32) << 16) + uint32_t(buf * C::N + side * WC);
@@ -591,13 +651,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_ns_product(const __grid_constan
         }
         if (k1 == ksteps) {
 #pragma unroll 1
-          for (int c = 0; c < WC; c += 16) {
-            if (c) ask<MODE>(a, p, col, c, beside);
+          for (int c = 0; ok && c < WC; c += 32) {
+            if (c) ask<MODE>(maps, a, w, t.z, row, col + c);
             __syncwarp();
-            uint32_t v[16];
-            tc_ld16(taddr + c, v);
-            tc_wait_ld();
-            finish<MODE, TALL, NPROD>(a, t, p, col, c, lane, v, beside, turn);
+            ok = finish<MODE, TALL, NPROD>(maps, a, w, t, row, col + c, taddr + c);
           }
         }
         tc_fence_before();
@@ -606,6 +663,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_ns_product(const __grid_constan
         k0 = k1;
       }
     }
+    if (!ok) {
+      if (lane == 0) raise(a.status, XRL_ERR_TIMEOUT);
+      let_copies_land();
+    }
+    if (lane == 0) tma_wait_all();
   }
   tc_fence_before();
   __syncwarp();
@@ -620,16 +682,17 @@ __global__ void __launch_bounds__(kThreads, 1) k_ns_product(const __grid_constan
 }
 
 // ---- host side ---------------------------------------------------------------------------------------------------
-// fp16 matrices [batch][rows][cols] with rows ld entries apart, box of 64 columns by box_rows rows, 128-byte swizzle
-bool make_map3(CUtensorMap* m, const void* ptr, int batch, int rows, int cols, int64_t ld, uint32_t box_rows) {
+// fp16 matrices [batch][rows][cols] with rows ld entries apart, box of 64 columns by box_rows rows, 128-byte swizzle; or the
+// epilogue's pieces of 32 x 32, 64-byte swizzle
+bool make_map3(CUtensorMap* m, const void* ptr, int batch, int rows, int cols, int64_t ld, uint32_t box_rows, bool piece = false) {
   EncodeTiledFn fn = encode_fn();
   if (!fn) return false;
   cuuint64_t dims[3] = {cuuint64_t(cols), cuuint64_t(rows), cuuint64_t(batch)};
   cuuint64_t strides[2] = {cuuint64_t(ld) * 2, cuuint64_t(ld) * 2 * cuuint64_t(rows)};
-  cuuint32_t box[3] = {KCH, box_rows, 1};
+  cuuint32_t box[3] = {cuuint32_t(piece ? 32 : KCH), box_rows, 1};
   cuuint32_t estr[3] = {1, 1, 1};
   return fn(m, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<void*>(ptr), dims, strides, box, estr,
-            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, piece ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 // fp16 operands as matrices of the workspace
@@ -666,23 +729,30 @@ bool launch_tiles(const Maps& maps, NsArgs a, int batch, cudaStream_t st) {
   return cudaLaunchKernelEx(&cfg, k_ns_product<CTAS, COLS, MODE, TALL, NPROD>, maps, a) == cudaSuccess;
 }
 
-// Tiles of a product: of 256 rows by a pair of CTAs where those keep most SMs busy, else of 128 x 128, else of 128 x 64
+bool make_pieces(CUtensorMap* hi, CUtensorMap* lo, const Operand& o, int batch) {
+  return make_map3(hi, o.p.hi, batch, o.rows, o.cols, o.ld, 32, true) && make_map3(lo, o.p.lo, batch, o.rows, o.cols, o.ld, 32, true);
+}
+
+// Tiles of a product: of 256 rows by a pair of CTAs where those keep most SMs busy, else of 128 x 128 (one product), else of
+// 128 x 64
 template <int MODE, bool TALL, int NPROD>
-bool launch_product(const Operand& left, const Operand& right, const NsArgs& a, int batch, cudaStream_t st) {
+bool launch_product(const Operand& left, const Operand& right, const Operand* in, const Operand& out, const NsArgs& a, int batch,
+                    cudaStream_t st) {
   constexpr bool A_MN = MODE == GRAM && TALL, B_MN = A_MN || (MODE == APPLY && !TALL);
   constexpr int WIDE = NPROD == 1 ? 256 : 128;           // columns of a pair's tile
   auto tiles = [&](int m, int n) {
     const int64_t tm = (a.m + m - 1) / m, tn = (a.n + n - 1) / n;
     return (MODE == APPLY ? tm * tn : tm * (tm + 1) / 2 * (m / n)) * batch;
   };
-  const int kind = tiles(256, WIDE) >= 60 ? 2 : tiles(128, 128) >= 100 ? 1 : 0;
+  const int kind = tiles(256, WIDE) >= 60 ? 2 : NPROD == 1 && tiles(128, 128) >= 100 ? 1 : 0;
   const int outer = kind == 2 ? WIDE / 2 : kind == 1 ? 128 : 64;
   Maps maps;
   if (!make_operand(&maps.a_hi, &maps.a_lo, left, batch, A_MN, kRows, NPROD > 1) ||
-      !make_operand(&maps.b_hi, &maps.b_lo, right, batch, B_MN, outer, NPROD > 1))
+      !make_operand(&maps.b_hi, &maps.b_lo, right, batch, B_MN, outer, NPROD > 1) ||
+      (in && !make_pieces(&maps.in_hi, &maps.in_lo, *in, batch)) || !make_pieces(&maps.out_hi, &maps.out_lo, out, batch))
     return false;
   if (kind == 2) return launch_tiles<2, WIDE, MODE, TALL, NPROD>(maps, a, batch, st);
-  if (kind == 1) return launch_tiles<1, 128, MODE, TALL, NPROD>(maps, a, batch, st);
+  if (NPROD == 1 && kind == 1) return launch_tiles<1, NPROD == 1 ? 128 : 64, MODE, TALL, NPROD>(maps, a, batch, st);
   return launch_tiles<1, 64, MODE, TALL, NPROD>(maps, a, batch, st);
 }
 
@@ -708,8 +778,8 @@ NsSpace layout(void* ws, int batch, int rows, int cols) {
   s.ldm = (int64_t(small) + kPad - 1) / kPad * kPad;
   s.status = reinterpret_cast<int32_t*>(take(4));
   s.partial = reinterpret_cast<double*>(take(size_t(batch) * kNormBlocks * 8));
-  s.dA = reinterpret_cast<float*>(take(size_t(batch) * small * 4));
-  s.dB = reinterpret_cast<float*>(take(size_t(batch) * small * 4));
+  s.dA = reinterpret_cast<float*>(take(size_t(batch) * s.ldm * 4));
+  s.dB = reinterpret_cast<float*>(take(size_t(batch) * s.ldm * 4));
   const size_t xb = size_t(batch) * rows * s.ldx * 2, mb = size_t(batch) * small * s.ldm * 2;
   for (Half2* p : {&s.x[0], &s.x[1]}) {
     p->hi = reinterpret_cast<__half*>(take(xb));
@@ -739,40 +809,35 @@ bool run_steps(int batch, int rows, int cols, const void* grad, int64_t ld, int6
   NsArgs gram = {};
   gram.m = gram.n = small;
   gram.k = large;
-  gram.ld_in = gram.ld_out = s.ldm;
+  gram.diag_stride = s.ldm;
   gram.descale = 1.f / (xs * xs);
   gram.gain = kGramScale / (xs * xs);
   gram.diag_in = s.dA;
   gram.diag_out = s.dA;
-  gram.out = s.f;
   gram.status = status;
   NsArgs poly = gram, apply = gram;
   poly.k = small;
   poly.descale = 1.f / (kGramScale * kGramScale);
   poly.gain = kC / kGramScale;
-  poly.in = s.f;
-  poly.out = s.b;
   poly.diag_out = s.dB;
   apply.m = rows;
   apply.n = cols;
   apply.k = small;
   apply.gain = 1.f / kGramScale;
   apply.unscale = 1.f / xs;
-  apply.ld_in = apply.ld_out = s.ldx;
   apply.diag_in = s.dB;
 
   const Operand f = {s.f, small, small, s.ldm}, b = {s.b, small, small, s.ldm};
   for (int i = 0; i < steps; ++i) {
-    const Operand x = {s.x[i & 1], rows, cols, s.ldx};
-    apply.in = x.p;
-    apply.out = s.x[(i + 1) & 1];
+    const Operand x = {s.x[i & 1], rows, cols, s.ldx}, next = {s.x[(i + 1) & 1], rows, cols, s.ldx};
     if (i == steps - 1) {
       apply.user = out;
       apply.user_ld = out_ld;
       apply.user_batch = out_bs;
     }
-    if (!launch_product<GRAM, TALL, NPROD>(x, x, gram, batch, st) || !launch_product<POLY, false, NPROD>(f, f, poly, batch, st) ||
-        !launch_product<APPLY, TALL, NPROD>(TALL ? x : b, TALL ? b : x, apply, batch, st))
+    if (!launch_product<GRAM, TALL, NPROD>(x, x, nullptr, f, gram, batch, st) ||
+        !launch_product<POLY, false, NPROD>(f, f, &f, b, poly, batch, st) ||
+        !launch_product<APPLY, TALL, NPROD>(TALL ? x : b, TALL ? b : x, &x, next, apply, batch, st))
       return false;
   }
   return true;
