@@ -146,12 +146,12 @@ constexpr int kBlockBytes = 32 * 32 * 2; // a 32 x 32 piece of an epilogue warp:
 // and N / 2 of the right one, so a tile of 256 x 256 asks half of what four of 128 x 128 do of L2.
 // CHUNK: stages whose products stay in one accumulator.  The tensor cores cut the sum after each instruction instead of
 // rounding it, which shrinks a sum of n instructions by about n / 4 units in its last place (fp32, 32 x 8,192 in one
-// accumulator: 4e-5 of the update).  fp32 updates therefore add the accumulators of 128 entries of the reduction in registers,
+// accumulator: 4e-5 of the update).  fp32 updates therefore add the accumulators of 256 entries of the reduction in registers,
 // and issue the small products of a stage first, onto a small sum.
 template <int CTAS, int COLS, int NPROD> struct Cfg {
   static constexpr int M = CTAS * kRows, N = COLS;
   static constexpr int SUB = M / N;                       // tiles side by side in a square of M x M
-  static constexpr int CHUNK = NPROD == 1 ? 1 << 30 : 2;
+  static constexpr int CHUNK = NPROD == 1 ? 1 << 30 : 4;
   static constexpr int B_ROWS = N / CTAS;
   static constexpr int A_BYTES = kRows * kStep * 2, B_BYTES = B_ROWS * kStep * 2;
   static constexpr int PARTS = NPROD == 1 ? 1 : 2;        // hi; hi and lo
@@ -273,13 +273,6 @@ template <int M, int N, bool SYM> __device__ __forceinline__ Tile tile_of(const 
   return r;
 }
 
-__device__ __forceinline__ void tc_ld16(uint32_t taddr, uint32_t (&r)[16]) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
-      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
-        "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]) : "r"(taddr) : "memory");
-}
 __device__ __forceinline__ void tc_st16(uint32_t taddr, const float* r) {
   const uint32_t* u = reinterpret_cast<const uint32_t*>(r);
   asm volatile(
@@ -632,30 +625,32 @@ __global__ void __launch_bounds__(kThreads, 1) k_ns_product(const __grid_constan
         const uint32_t taddr = tmem_base + (uint32_t(q * 32) << 16) + uint32_t(buf * C::N + side * WC);
         if (NPROD > 1 && ksteps > C::CHUNK) {
           // the sums so far; with the last accumulator they go back into its place
-#pragma unroll
-          for (int c = 0; c < WC; c += 16) {
-            uint32_t v[16];
-            tc_ld16(taddr + c, v);
+          uint32_t v[NPROD == 1 ? 1 : WC];
+          if constexpr (NPROD > 1) {
+            static_assert(WC == 32, "one load");
+            tc_ld32(taddr, v);
             tc_wait_ld();
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              float& x = sum[NPROD == 1 ? 0 : c + i];
-              x = (k0 == 0 ? 0.f : x) + __uint_as_float(v[i]);
-            }
           }
-          if (k1 == ksteps) {
-#pragma unroll
-            for (int c = 0; c < WC; c += 16) tc_st16(taddr + c, sum + (NPROD == 1 ? 0 : c));
-            asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
-          }
-        }
-        if (k1 == ksteps) {
-#pragma unroll 1
-          for (int c = 0; ok && c < WC; c += 32) {
-            if (c) ask<MODE>(maps, a, w, t.z, row, col + c);
+          if (k1 < ksteps) {             // the accumulator is free before its values are added
+            tc_fence_before();
             __syncwarp();
-            ok = finish<MODE, TALL, NPROD>(maps, a, w, t, row, col + c, taddr + c);
+            if (lane == 0) arrive_first<CTAS>(bar_acc_empty(buf));
           }
+#pragma unroll
+          for (int i = 0; i < (NPROD == 1 ? 1 : WC); ++i) sum[i] = (k0 == 0 ? 0.f : sum[i]) + __uint_as_float(v[i]);
+          k0 = k1;
+          if (k1 < ksteps) continue;
+          if constexpr (NPROD > 1) {
+#pragma unroll
+            for (int c = 0; c < WC; c += 16) tc_st16(taddr + c, sum + c);
+          }
+          asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+        }
+#pragma unroll 1
+        for (int c = 0; ok && c < WC; c += 32) {
+          if (c) ask<MODE>(maps, a, w, t.z, row, col + c);
+          __syncwarp();
+          ok = finish<MODE, TALL, NPROD>(maps, a, w, t, row, col + c, taddr + c);
         }
         tc_fence_before();
         __syncwarp();
