@@ -333,7 +333,7 @@ xrl_status xrl_gae(int32_t device, int32_t num_steps, int32_t num_trajectories, 
  *               vocab) largest logits of the support in falling order, equal ones by rising index, and their ln p; -1 and
  *               -infinity where the support has fewer
  * A row with a NaN or +infinity in its support gives NaN in logp, entropy, l and top_logp; its alternatives are the best of
- * its other entries.  Sums are added in an order that depends on the sizes alone.  Needs no context; one launch; captures
+ * its other entries.  The order of a row's sum depends on the sizes and on where the row lies on its 16-byte boundary alone.  Needs no context; one launch; captures
  * into a CUDA graph; nothing is allocated.  Errors: INVALID_ARG, UNSUPPORTED (num_top), CUDA. */
 #define XRL_MAX_TOP 32
 xrl_status xrl_logprob(int32_t device, int32_t dtype, int32_t rows, int32_t vocab, const void* logits, int64_t row_stride,

@@ -17,9 +17,13 @@ constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kNegInf = -INFINITY;
 constexpr unsigned kAll = 0xFFFFFFFFu;
 constexpr int kMostTop = 32;             // alternatives: one lane of a warp each
-// What -infinity becomes while a row is summed: 2^(kFloor c - r) is 0 and a product with it finite.  A row without a logit
-// above it (nothing in its support, or only values like the type's lowest) is done again by careful_row.
-constexpr float kFloor = -1e30f;
+// What -infinity becomes in the gradient, where p = 2^((x - m) c - l) is 0 for it and a product with it finite.  (A bf16
+// number, 0xF149.)
+constexpr float kFloor = -9.953287e29f;
+// The sums of a row are taken relative to r = c m rounded, which all terms share: as long as |c m| is at most 2^24 that is
+// off by 1 at most and cancels.  Logits below -2^23 / c count as that (their share is 0 all the same: a row whose largest
+// is below -2^22 / c, or above 2^24 / c, is done again by careful_row).
+constexpr float kLowest = -8388608.f, kLow = -4194304.f, kHigh = 16777216.f;
 
 __device__ __forceinline__ float ex2(float x) {
   float y;
@@ -30,6 +34,39 @@ __device__ __forceinline__ float max_nan(float a, float b) {     // a number tha
   float y;
   asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
   return y;
+}
+// two fp32 numbers in one register pair, and the instructions that take both at once
+typedef unsigned long long f32x2;
+__device__ __forceinline__ f32x2 pair(float lo, float hi) {
+  f32x2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ void unpair(f32x2 v, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
+  f32x2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
+  f32x2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) {
+  f32x2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint32_t max_bf16x2(uint32_t a, uint32_t b) {         // numbers that are none are passed over
+  uint32_t r;
+  asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+__device__ __forceinline__ uint32_t max_nan_bf16x2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
 }
 template <typename T> __device__ __forceinline__ float load1(const T* p) { return to_float(__ldg(p)); }
 template <> __device__ __forceinline__ float load1<bf16>(const bf16* p) {
@@ -278,7 +315,7 @@ __device__ __forceinline__ float float_of(uint32_t key) {
   return __uint_as_float(key & 0x80000000u ? key & 0x7FFFFFFFu : ~key);
 }
 
-// A row without a logit above kFloor, or with numbers that are none: largest first, then the sums of differences.
+// A row whose logits are too far from 0 for the above: largest first, then the sums of differences.
 template <typename T, int THREADS>
 __device__ __noinline__ void careful_row(const RowArgs& a, bool masked, int64_t row, float* red, Sums& out) {
   const Row<T> r(a, row, masked);
@@ -336,217 +373,248 @@ __device__ __forceinline__ int32_t remote_i(uint32_t at) {
   return v;
 }
 
-// the sums of U vectors of a thread, from the raw 16-byte pieces
+// The logits of U vectors for the arithmetic, none below `floor`: N pairs of fp32 numbers; and the largest of them as they were
 template <int U>
-__device__ __forceinline__ void add_chunk(Sums& q, const uint4 (&v)[U], float c, const bf16*) {
-  float f[U * 8];
+__device__ __forceinline__ float spread(const uint4 (&v)[U], f32x2 (&f)[U * 4], float floor, const bf16*) {
+  const uint32_t f2 = pack_bf16x2(floor, floor);
+  const uint32_t* w = reinterpret_cast<const uint32_t*>(v);
+  uint32_t m = w[0];
 #pragma unroll
-  for (int u = 0; u < U; ++u) {
-    float g[8];
-    unpack(v[u], g);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) f[8 * u + i] = max_nan(g[i], kFloor);
-  }
-  float m = q.m;
-#pragma unroll
-  for (int i = 0; i < U * 8; ++i) m = fmaxf(m, f[i]);
-  const float r = m * c, d = q.r - r, e = ex2(d);
-  q.t = fmaf(d, q.s, q.t) * e;
-  q.s *= e;
-  q.m = m;
-  q.r = r;
-#pragma unroll
-  for (int i = 0; i < U * 8; ++i) {
-    const float y = fmaf(f[i], c, -r), p = ex2(y);
-    q.s += p;
-    q.t = fmaf(p, y, q.t);
-  }
-}
-template <int U>
-__device__ __forceinline__ void add_chunk(Sums& q, const uint4 (&v)[U], float c, const float*) {
-  float f[U * 4];
-#pragma unroll
-  for (int u = 0; u < U; ++u) {
-    float g[4];
-    unpack(v[u], g);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) f[4 * u + i] = max_nan(g[i], kFloor);
-  }
-  float m = q.m;
-#pragma unroll
-  for (int i = 0; i < U * 4; ++i) m = fmaxf(m, f[i]);
-  const float r = m * c, d = q.r - r, e = ex2(d);
-  q.t = fmaf(d, q.s, q.t) * e;
-  q.s *= e;
-  q.m = m;
-  q.r = r;
+  for (int i = 1; i < U * 4; ++i) m = max_bf16x2(m, w[i]);
 #pragma unroll
   for (int i = 0; i < U * 4; ++i) {
-    const float y = fmaf(f[i], c, -r), p = ex2(y);
-    q.s += p;
-    q.t = fmaf(p, y, q.t);
+    const uint32_t x = max_nan_bf16x2(w[i], f2);
+    f[i] = pair(__uint_as_float(x << 16), __uint_as_float(x & 0xFFFF0000u));
   }
+  return fmaxf(__uint_as_float(m << 16), __uint_as_float(m & 0xFFFF0000u));
+}
+template <int U>
+__device__ __forceinline__ float spread(const uint4 (&v)[U], f32x2 (&f)[U * 2], float floor, const float*) {
+  const uint32_t* w = reinterpret_cast<const uint32_t*>(v);
+  float m = __uint_as_float(w[0]);
+#pragma unroll
+  for (int i = 1; i < U * 4; ++i) m = fmaxf(m, __uint_as_float(w[i]));
+#pragma unroll
+  for (int i = 0; i < U * 2; ++i)
+    f[i] = pair(max_nan(__uint_as_float(w[2 * i]), floor), max_nan(__uint_as_float(w[2 * i + 1]), floor));
+  return m;
+}
+// adds them to a thread's sums
+template <typename T, int U>
+__device__ __forceinline__ void add_chunk(Sums& q, const uint4 (&v)[U], float c, float floor) {
+  constexpr int P = U * Vec<T>::N / 2;
+  f32x2 f[P];
+  const float m = fmaxf(q.m, spread<U>(v, f, floor, static_cast<const T*>(nullptr)));
+  const float r = fmaxf(m, floor) * c, d = q.r - r, e = ex2(d);
+  const f32x2 cc = pair(c, c), rr = pair(-r, -r);
+  f32x2 s[2] = {pair(q.s * e, 0.f), 0ull}, t[2] = {pair(fmaf(d, q.s, q.t) * e, 0.f), 0ull};
+#pragma unroll
+  for (int i = 0; i < P; ++i) {
+    const f32x2 y = fma2(f[i], cc, rr);
+    float y0, y1;
+    unpair(y, y0, y1);
+    const f32x2 p = pair(ex2(y0), ex2(y1));
+    s[i & 1] = add2(s[i & 1], p);
+    t[i & 1] = fma2(p, y, t[i & 1]);
+  }
+  float a, b;
+  unpair(add2(s[0], s[1]), a, b);
+  q.s = a + b;
+  unpair(add2(t[0], t[1]), a, b);
+  q.t = a + b;
+  q.m = m;
+  q.r = r;
 }
 
-// What a CTA leaves for the first one of its cluster
-struct Part {
-  Sums sums;
-  float v[kMostTop];
-  int32_t i[kMostTop];
+// ---- the best k of a CTA's part of a row -----------------------------------------------------------------------
+// Candidates in shared memory: the k best of n <= THREADS, by counting for each how many are better
+template <int THREADS> struct Candidates {
+  float v[THREADS];
+  int32_t i[THREADS];
+  float best_v[kMostTop];
+  int32_t best_i[kMostTop];
+  int n;
 };
+template <int THREADS> __device__ __forceinline__ void rank_candidates(Candidates<THREADS>& s, int n, int k) {
+  if (threadIdx.x < kMostTop) { s.best_v[threadIdx.x] = kNegInf; s.best_i[threadIdx.x] = INT32_MAX; }
+  __syncthreads();
+  if (int(threadIdx.x) < n) {
+    const float v = s.v[threadIdx.x];
+    const int32_t i = s.i[threadIdx.x];
+    int rank = 0;
+    for (int j = 0; j < n; ++j) rank += better(s.v[j], s.i[j], v, i) ? 1 : 0;
+    if (rank < k && v > kNegInf) { s.best_v[rank] = v; s.best_i[rank] = i; }
+  }
+  __syncthreads();
+}
+
+// A thread's largest logit (thread_max) is known.  At least k threads hold one of `bound` or more, so the k best are no
+// less; few other logits are, and only the threads whose largest is that high have any.  Their vectors are read again, spread
+// over the lanes of their warp, and what reaches the bound is ranked.  Where that is more than one entry per thread of
+// the CTA (equal logits everywhere, or fewer than k threads with any) each warp keeps a sorted list of its whole part instead.
+template <typename T, int THREADS, bool MASK>
+__device__ __forceinline__ void best_of_part(const Row<T>& r, int v0, int v1, bool edges, float thread_max, float part_max, int k,
+                                             Candidates<THREADS>& s, uint32_t* red) {
+  constexpr int N = Vec<T>::N, U = 4, W = THREADS / 32, GROUP = THREADS / 32;
+  static_assert(GROUP <= 32, "32 groups of threads");
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const uint32_t mine = key_of(thread_max);
+  uint32_t g = mine;
+#pragma unroll
+  for (int d = 1; d < GROUP; d <<= 1) g = max(g, __shfl_xor_sync(kAll, g, d));
+  if (threadIdx.x % GROUP == 0) red[threadIdx.x / GROUP] = g;
+  if (threadIdx.x == 0) s.n = 0;
+  __syncthreads();
+  // 32 groups, each with a thread at `lo` or above
+  uint32_t lo = __reduce_min_sync(kAll, red[lane]), hi = key_of(part_max);
+  while (lo < hi) {
+    const uint32_t mid = lo + (hi - lo + 1) / 2;
+    const int cnt = __syncthreads_count(mine >= mid);
+    if (cnt >= k) {
+      lo = mid;
+      if (cnt <= k + k / 2) break;
+    } else {
+      hi = mid - 1;
+    }
+  }
+  const float bound = float_of(lo);
+  const unsigned flags = __ballot_sync(kAll, thread_max > kNegInf && mine >= lo);
+  const int iters = (v1 - v0 + THREADS - 1) / THREADS, items = __popc(flags) * iters;
+  auto put = [&](float v, int32_t i) {
+    if (v >= bound && v > kNegInf) {
+      const int at = atomicAdd(&s.n, 1);
+      if (at < THREADS) { s.v[at] = v; s.i[at] = i; }
+    }
+  };
+  for (int i = lane; i < items; i += 32) {
+    const int j = v0 + warp * 32 + __fns(flags, 0, i / iters + 1) + (i % iters) * THREADS;
+    if (j < v1) {
+      const uint4 v = r.template vec<MASK>(j);
+      float f[N];
+      unpack(v, f);
+#pragma unroll
+      for (int e = 0; e < N; ++e) put(f[e], r.head + j * N + e);
+    }
+  }
+  if (edges && threadIdx.x < 16) {
+    const int j = r.edge(threadIdx.x);
+    if (j >= 0) put(r.at(j), j);
+  }
+  __syncthreads();
+  int n = s.n;
+  if (n > THREADS) {
+    Best mine_b, last;
+    for (int j0 = v0 + warp * 32; j0 < v1; j0 += U * THREADS) {
+      uint4 v[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int j = j0 + u * THREADS + lane;
+        v[u] = j < v1 ? r.template vec<MASK>(j) : Vec<T>::none();
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        float f[N];
+        unpack(v[u], f);
+#pragma unroll
+        for (int i = 0; i < N; ++i) offer(mine_b, last, f[i], r.head + (j0 + u * THREADS + lane) * N + i, k, lane);
+      }
+    }
+    if (edges && warp == 0) {
+      const int j = lane < 16 ? r.edge(lane) : -1;
+      offer(mine_b, last, j >= 0 ? r.at(j) : kNegInf, j, k, lane);
+    }
+    s.v[threadIdx.x] = mine_b.v;
+    s.i[threadIdx.x] = mine_b.i;
+    __syncthreads();
+    n = THREADS;
+  }
+  rank_candidates<THREADS>(s, n, k);
+}
 
 template <typename T, int THREADS, bool MASK, bool TOP>
-__global__ void __launch_bounds__(THREADS) k_logprob_cta(RowArgs a, RowOut o, int parts) {
+__global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_logprob_cta(RowArgs a, RowOut o, int parts) {
   enter();
-  constexpr int N = Vec<T>::N, U = 4, W = THREADS / 32;
+  constexpr int U = 4, W = THREADS / 32;
   __shared__ Sums s_sums[W];
   __shared__ float s_red[64];
-  __shared__ float s_v[TOP ? W * kMostTop : 1];
-  __shared__ int32_t s_i[TOP ? W * kMostTop : 1];
-  __shared__ Part s_part;
+  __shared__ Candidates<TOP ? THREADS : 32> s_best;
+  __shared__ Sums s_part;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int64_t row = int64_t(blockIdx.x) / parts;
   const int part = parts > 1 ? int(cluster_rank()) : 0;
   const Row<T> r(a, row, MASK);
   const float c = a.scale * kLog2e;
   const int v0 = int(int64_t(r.vecs) * part / parts), v1 = int(int64_t(r.vecs) * (part + 1) / parts);
+  // (as a bf16 number, which it is for both types; rounded, it is within 2^-9 of itself)
+  const float floor = to_float(bf16(kLowest / c));
+  const Sums zero = {kNegInf, floor * c, 0.f, 0.f};
 
-  Sums q = {kFloor, kFloor * c, 0.f, 0.f};
+  Sums q = zero;
   for (int j = v0 + threadIdx.x; j < v1; j += U * THREADS) {
     uint4 v[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) v[u] = j + u * THREADS < v1 ? r.template vec<MASK>(j + u * THREADS) : Vec<T>::none();
-    add_chunk<U>(q, v, c, static_cast<const T*>(nullptr));
+    add_chunk<T, U>(q, v, c, floor);
   }
+  const float thread_max = q.m;          // (of its whole vectors)
   if (part == 0 && threadIdx.x < 16) {
     const int j = r.edge(threadIdx.x);
     if (j >= 0) {
-      const float x = max_nan(r.at(j), kFloor), m = fmaxf(q.m, x), y = fmaf(x, c, -(m * c)), p = ex2(y);
-      q = join(q, Sums{m, m * c, p, p * y});
+      const float x = r.at(j), z = max_nan(x, floor), e = fmaxf(x, floor) * c, y = fmaf(z, c, -e), p = ex2(y);
+      q = join(q, Sums{fmaxf(x, kNegInf), e, p, p * y});
     }
   }
-  const float thread_max = q.m;
   q = join_warp(q);
   if (lane == 0) s_sums[warp] = q;
   __syncthreads();
-  q = s_sums[lane < W ? lane : 0];
-  if (lane >= W) q = {kFloor, kFloor * c, 0.f, 0.f};
+  q = lane < W ? s_sums[lane] : zero;
   q = join_warp(q);
 
-  if (TOP) {
-    // k threads at least hold a logit of `bound` or more, so the k best are no less; the few threads whose largest is that
-    // high are walked again, each by its warp.  Where that is many of them (fewer than k threads above the floor, or equal
-    // logits everywhere) the whole part is.
-    const int k = o.top;
-    int at_lo = THREADS;                                        // threads whose largest is `lo` or more: k at least
-    uint32_t lo = key_of(kFloor), hi = key_of(q.m);
-    const uint32_t mine_key = key_of(thread_max);
-    while (lo < hi) {
-      const uint32_t mid = lo + (hi - lo + 1) / 2;
-      const int cnt = __syncthreads_count(mine_key >= mid);
-      if (cnt >= k) {
-        lo = mid;
-        at_lo = cnt;
-        if (cnt <= k + k / 2) break;
-      } else {
-        hi = mid - 1;
-      }
-    }
-    const float bound = float_of(lo);
-    const bool all = !(bound > kFloor);
-    Best mine, last;
-    if (all || at_lo > 4 * kMostTop) {
-      for (int j0 = v0 + warp * 32; j0 < v1; j0 += U * THREADS) {
-        uint4 v[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-          const int j = j0 + u * THREADS + lane;
-          v[u] = j < v1 ? r.template vec<MASK>(j) : Vec<T>::none();
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-          float f[N];
-          unpack(v[u], f);
-#pragma unroll
-          for (int i = 0; i < N; ++i)
-            offer(mine, last, all || f[i] >= bound ? f[i] : kNegInf, r.head + (j0 + u * THREADS + lane) * N + i, k, lane);
-        }
-      }
-    } else {
-      unsigned todo = __ballot_sync(kAll, thread_max >= bound);
-      while (todo) {
-        const int from = __ffs(todo) - 1;
-        todo &= todo - 1;
-        for (int j0 = v0 + warp * 32 + from; j0 < v1; j0 += 32 * THREADS) {
-          const int j = j0 + lane * THREADS;
-          const uint4 v = j < v1 ? r.template vec<MASK>(j) : Vec<T>::none();
-          float f[N];
-          unpack(v, f);
-#pragma unroll
-          for (int i = 0; i < N; ++i) offer(mine, last, f[i] >= bound ? f[i] : kNegInf, r.head + j * N + i, k, lane);
-        }
-      }
-    }
-    if (part == 0 && warp == 0) {
-      const int j = lane < 16 ? r.edge(lane) : -1;
-      offer(mine, last, j >= 0 ? r.at(j) : kNegInf, j, k, lane);
-    }
-    s_v[warp * kMostTop + lane] = mine.v;
-    s_i[warp * kMostTop + lane] = mine.i;
-    __syncthreads();
-    if (warp == 0) {
-      for (int w = 1; w < W; ++w)
-        offer(mine, last, lane < k ? s_v[w * kMostTop + lane] : kNegInf, s_i[w * kMostTop + lane], k, lane);
-      s_part.v[lane] = mine.v;
-      s_part.i[lane] = mine.i;
-    }
-  }
+  if (TOP) best_of_part<T, TOP ? THREADS : 32, MASK>(r, v0, v1, part == 0, thread_max, q.m, o.top, s_best, reinterpret_cast<uint32_t*>(s_red));
   if (parts > 1) {
-    if (threadIdx.x == 0) s_part.sums = q;
+    if (threadIdx.x == 0) s_part = q;
     cluster_arrive_wait();
     if (part == 0) {
       if (lane > 0 && lane < parts) {
-        const uint32_t at = remote(&s_part.sums, lane);
+        const uint32_t at = remote(&s_part, lane);
         q = {remote_f(at), remote_f(at + 4), remote_f(at + 8), remote_f(at + 12)};
       } else if (lane >= parts) {
-        q = {kFloor, kFloor * c, 0.f, 0.f};
+        q = zero;
       }
       q = join_warp(q);
-      if (TOP && warp == 0) {
-        Best mine, last;
-        mine.v = s_part.v[lane];
-        mine.i = s_part.i[lane];
-        last.v = __shfl_sync(kAll, mine.v, o.top - 1);
-        last.i = __shfl_sync(kAll, mine.i, o.top - 1);
-        for (int p = 1; p < parts; ++p) {
-          const float v = remote_f(remote(&s_part.v[lane], p));
-          const int32_t i = remote_i(remote(&s_part.i[lane], p));
-          offer(mine, last, lane < o.top ? v : kNegInf, i, o.top, lane);
+      if (TOP) {
+        const int p = threadIdx.x / kMostTop, e = threadIdx.x % kMostTop;
+        float v = kNegInf;
+        int32_t i = INT32_MAX;
+        if (p < parts) {
+          v = remote_f(remote(&s_best.best_v[e], p));
+          i = remote_i(remote(&s_best.best_i[e], p));
         }
-        s_v[lane] = mine.v;
-        s_i[lane] = mine.i;
+        s_best.v[threadIdx.x] = v;
+        s_best.i[threadIdx.x] = i;
       }
     }
-    cluster_arrive_wait();               // nobody leaves while its shared memory is read
+    cluster_arrive_wait();               // nobody leaves, and nothing is written again, while it is read
     if (part != 0) return;
-  } else if (TOP && warp == 0) {
-    s_v[lane] = s_part.v[lane];
-    s_i[lane] = s_part.i[lane];
+    if (TOP) rank_candidates(s_best, parts * kMostTop, o.top);
   }
   RowNorm n;
   float entropy;
-  if (q.m > kFloor && q.s == q.s) {
-    n = norm_of(q, c);
-    entropy = entropy_of(q);
-  } else {
+  if (q.m > kNegInf && q.m < INFINITY && !(q.m * c > kLow && q.m * c < kHigh)) {
     Sums z;
     careful_row<T, THREADS>(a, MASK, row, s_red, z);
-    const bool empty = z.s == 0.f;
-    n = {z.m, empty ? kNegInf : kLn2 * log2f(z.s)};
-    entropy = empty ? 0.f : entropy_of(z);
+    n = {z.m, kLn2 * log2f(z.s)};
+    entropy = entropy_of(z);
+  } else if (q.m > kNegInf || q.s != q.s) {
+    n = norm_of(q, c);
+    if (q.s != q.s) n.l = NAN;
+    entropy = entropy_of(q);
+  } else {
+    n = {kNegInf, kNegInf};
+    entropy = 0.f;
   }
   if (threadIdx.x == 0) write_row<T>(a, o, row, n, entropy);
-  if (TOP && warp == 0) write_top(a, o, row, n, Best{s_v[lane], s_i[lane]}, lane);
+  if (TOP && warp == 0) write_top(a, o, row, n, Best{s_best.best_v[lane], s_best.best_i[lane]}, lane);
 }
 
 // ---- gradient ---------------------------------------------------------------------------------------------------
@@ -555,26 +623,46 @@ struct GradArgs {
   void* grad;
   int64_t grad_stride;
 };
+// One entry as the formula says it; what the fast form below leaves out
 struct RowGrad {
-  float m, c, l2, dl, dh, ent, scale;    // l2: l in powers of two; dl, dh times the scale
+  float m, c, l2, dl, dh, ent;           // l2: l in powers of two; dl, dh times the scale
   int32_t t;
-  // lp = ln p, p = exp(lp): in the support
   __device__ __forceinline__ float operator()(float x, int j) const {
     const float y = fmaf(x - m, c, -l2), p = ex2(y);
     const float g = fmaf(dl, (j == t ? 1.f : 0.f) - p, p > 0.f || p != p ? -dh * p * fmaf(kLn2, y, ent) : 0.f);
     return x > kNegInf || x != x ? g : 0.f;
   }
 };
+template <typename T> __device__ __forceinline__ uint4 round_pairs(const f32x2* g);
+template <> __device__ __forceinline__ uint4 round_pairs<bf16>(const f32x2* g) {
+  float f[8];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) unpair(g[i], f[2 * i], f[2 * i + 1]);
+  return pack(f);
+}
+template <> __device__ __forceinline__ uint4 round_pairs<float>(const f32x2* g) {
+  float f[4];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) unpair(g[i], f[2 * i], f[2 * i + 1]);
+  return pack(f);
+}
+// A warp takes 32 x U vectors of a row at a time.  With p = 2^y the entry is p (A + B y), plus dl at the token:
+// A = -(dl + dh H), B = -dh ln 2.  -infinity becomes kFloor first, for which p is 0; rows where that does not do (a norm
+// or gradients that are not finite, logits all below the floor) go entry by entry.
 template <typename T, bool MASK>
 __global__ void __launch_bounds__(256) k_logprob_grad(RowArgs a, GradArgs g, int segs) {
   enter();
-  constexpr int N = Vec<T>::N, U = 4;
+  constexpr int N = Vec<T>::N, U = 4, P = N / 2;
   const int lane = threadIdx.x & 31;
   const int64_t items = a.rows * segs, step = int64_t(gridDim.x) * 8;
   for (int64_t item = int64_t(blockIdx.x) * 8 + (threadIdx.x >> 5); item < items; item += step) {
-    const int64_t row = item / segs;
+    const int64_t row = items <= INT32_MAX ? int64_t(uint32_t(item) / uint32_t(segs)) : item / segs;
     const int seg = int(item - row * segs);
     const Row<T> r(a, row, MASK);
+    const int j0 = seg * 32 * U + lane;
+    uint4 v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) v[u] = j0 + u * 32 < r.vecs ? r.template vec<MASK>(j0 + u * 32) : Vec<T>::none();
     T* out = static_cast<T*>(g.grad) + row * g.grad_stride;
     RowGrad f;
     const float2 n = __ldg(reinterpret_cast<const float2*>(g.norm) + row);
@@ -586,29 +674,70 @@ __global__ void __launch_bounds__(256) k_logprob_grad(RowArgs a, GradArgs g, int
     f.dh = g.dentropy ? a.scale * __ldg(g.dentropy + row) : 0.f;
     f.ent = g.dentropy ? __ldg(g.entropy + row) : 0.f;
     const bool whole = ((reinterpret_cast<uintptr_t>(out + r.head)) & 15) == 0;
-    const int j0 = seg * 32 * U + lane;
-    uint4 v[U];
+    const float A = -fmaf(f.dh, f.ent, f.dl), B = -f.dh * kLn2;
+    // (every product of the fast form is finite then)
+    const bool fast = f.m > kFloor && fabsf(A) + fabsf(B) * fmaf(fabsf(f.m) - kFloor, f.c, fabsf(f.l2)) < INFINITY;
+    if (fast) {
+      const f32x2 mm = pair(-f.m, -f.m), cc = pair(f.c, f.c), ll = pair(-f.l2, -f.l2), aa = pair(A, A), bb = pair(B, B);
 #pragma unroll
-    for (int u = 0; u < U; ++u) if (j0 + u * 32 < r.vecs) v[u] = r.template vec<MASK>(j0 + u * 32);
+      for (int u = 0; u < U; ++u) {
+        if (j0 + u * 32 >= r.vecs) break;
+        const int j = r.head + (j0 + u * 32) * N;
+        f32x2 x[P];
+        const uint4 one[1] = {v[u]};
+        spread<1>(one, x, kFloor, static_cast<const T*>(nullptr));
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int j = r.head + (j0 + u * 32) * N;
-      if (j0 + u * 32 < r.vecs) {
-        float x[N];
-        unpack(v[u], x);
-#pragma unroll
-        for (int i = 0; i < N; ++i) x[i] = f(x[i], j + i);
-        if (whole) {
-          *reinterpret_cast<uint4*>(out + j) = pack(x);
-        } else {
-#pragma unroll
-          for (int i = 0; i < N; ++i) out[j + i] = T(x[i]);
+        for (int i = 0; i < P; ++i) {
+          const f32x2 y = fma2(add2(x[i], mm), cc, ll);
+          float y0, y1;
+          unpair(y, y0, y1);
+          x[i] = mul2(pair(ex2(y0), ex2(y1)), fma2(y, bb, aa));
         }
+        if (uint32_t(f.t - j) < uint32_t(N)) {           // (a token outside the support has no share)
+          float z[N];
+          unpack(v[u], z);
+          bool kept = false;
+#pragma unroll
+          for (int i = 0; i < N; ++i) kept |= f.t - j == i && z[i] > kNegInf;
+#pragma unroll
+          for (int i = 0; i < P; ++i) {
+            float lo, hi;
+            unpair(x[i], lo, hi);
+            x[i] = pair(f.t - j == 2 * i && kept ? lo + f.dl : lo, f.t - j == 2 * i + 1 && kept ? hi + f.dl : hi);
+          }
+        }
+        const uint4 w = round_pairs<T>(x);
+        if (whole) {
+          *reinterpret_cast<uint4*>(out + j) = w;
+        } else {
+          const T* e = reinterpret_cast<const T*>(&w);
+#pragma unroll
+          for (int i = 0; i < N; ++i) out[j + i] = e[i];
+        }
+      }
+    } else {
+#pragma unroll 1
+      for (int u = 0; u < U; ++u) {
+        if (j0 + u * 32 >= r.vecs) break;
+        const int j = r.head + (j0 + u * 32) * N;
+        float x[N];
+        unpack(r.template vec<MASK>(j0 + u * 32), x);
+#pragma unroll
+        for (int i = 0; i < N; ++i) out[j + i] = T(f(x[i], j + i));
       }
     }
     if (seg == 0 && lane < 16) {
       const int j = r.edge(lane);
-      if (j >= 0) out[j] = T(f(r.at(j), j));
+      if (j >= 0) {
+        const float x = r.at(j);
+        float d = f(x, j);
+        if (fast) {                      // the same roundings as in a whole vector
+          const float y = fmaf(max_nan(x, kFloor) - f.m, f.c, -f.l2);
+          d = ex2(y) * fmaf(y, B, A);
+          if (j == f.t && x > kNegInf) d += f.dl;
+        }
+        out[j] = T(d);
+      }
     }
   }
 }
@@ -630,6 +759,16 @@ void launch_cluster(K kernel, unsigned grid, unsigned threads, unsigned cluster,
   cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
+#ifndef LP_THREADS
+#define LP_THREADS 512
+#endif
+constexpr int kThreads = LP_THREADS;
+template <typename T, bool MASK, int THREADS>
+void launch_cta(const RowArgs& a, const RowOut& o, int parts, cudaStream_t st) {
+  const unsigned grid = unsigned(a.rows * parts);
+  if (o.top) launch_cluster(k_logprob_cta<T, THREADS, MASK, true>, grid, THREADS, parts, st, a, o, parts);
+  else launch_cluster(k_logprob_cta<T, THREADS, MASK, false>, grid, THREADS, parts, st, a, o, parts);
+}
 template <typename T, bool MASK>
 void launch_rows(const RowArgs& a, const RowOut& o, cudaStream_t st) {
   if (a.vocab <= 1024) {
@@ -641,12 +780,9 @@ void launch_rows(const RowArgs& a, const RowOut& o, cudaStream_t st) {
     else launch(k_logprob_warp<T, 32, MASK>, grid, 128, 0, st, a, o);
     return;
   }
-  constexpr int THREADS = 512;
   int parts = 1;
   while (parts < 8 && a.rows * parts * 2 <= 2 * kNumSMs && a.vocab / (parts * 2) >= 4096) parts *= 2;
-  const unsigned grid = unsigned(a.rows * parts);
-  if (o.top) launch_cluster(k_logprob_cta<T, THREADS, MASK, true>, grid, THREADS, parts, st, a, o, parts);
-  else launch_cluster(k_logprob_cta<T, THREADS, MASK, false>, grid, THREADS, parts, st, a, o, parts);
+  launch_cta<T, MASK, kThreads>(a, o, parts, st);
 }
 template <typename T, bool MASK>
 void launch_grad(const RowArgs& a, const GradArgs& g, cudaStream_t st) {

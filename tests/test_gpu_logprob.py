@@ -156,6 +156,31 @@ def test_tokens_out_of_range_and_outputs_left_out():
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("vocab", [100, 1500, 70001])
+@pytest.mark.parametrize("scale", [1e-6, 1e-3, 0.37, 1.0, 3.3, 1e3, 1e6])
+def test_logits_of_every_size_and_scale(dtype, vocab, scale):
+    """Logits far from 0, and masks by large negative numbers of every size: the scaled ones are off by 2^-23 of themselves, an
+    exponential's argument by as much of what it is multiplied from."""
+    x, token, _, g = make(dtype, 24, vocab, 15)
+    x = x.float() / scale
+    for i, far in enumerate((1e3, 1e5, 1e7, 1e8, 1e9, 1e10, 1e12, 1e20, 1e30, 3e38)):
+        x[2 * i, torch.rand(vocab, device="cuda", generator=g) < 0.9] = -far
+        x[2 * i + 1] -= min(far / scale, 3e38)
+    x[20] += 1e3 / scale
+    x[21] += 1e9 / scale
+    x[22] += 1e30
+    x = x.clamp(-3e38, 3e38).to(DTYPES[dtype])
+    o, want = xrl.xrl_logprob(x, token, scale=scale, top=5), define(x, token, None, scale, 5)
+    e, l = sum_error(vocab), want["norm"][:, 1]
+    near(o["norm"][:, 0], want["norm"][:, 0], 0.0, "largest")
+    near(o["norm"][:, 1], l, e + 2.0 ** -23 * l.abs(), "l")
+    near(o["entropy"], want["entropy"], 4 * e * (1 + want["entropy"]), "entropy")
+    assert torch.equal(o["top_token"], want["top_token"])
+    fits = want["logp"].abs() < 3e38
+    near(o["logp"][fits], want["logp"][fits], (e + 2.0 ** -22 * (want["logp"].abs() + l.abs()))[fits], "logp")
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
 def test_the_same_bits_every_time_and_rows_alone(dtype):
     x, token, mask, _ = make(dtype, 33, 20011, 6)
     a = xrl.xrl_logprob(x, token, mask=mask, top=20)
@@ -242,6 +267,25 @@ def test_gradient_at_the_edges_of_the_range(dtype, vocab):
     assert bool((got[0] == 0).all()) and bool(torch.isnan(got[4:6]).all()) and float(got[7, 2]) == 0 and float(got[6, 1]) == 0
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_gradient_of_extreme_scales_and_gradients(dtype):
+    x, token, mask, g = make(dtype, 6, 1000, 14)
+    mask.scatter_(1, token.clamp(min=0).long()[:, None], 1)
+    x = x.clone()
+    x[:, 7] = -INF
+    for scale, big in ((1e6, 1e30), (1e-6, 1e30), (1e6, 1e-30)):
+        d, e = torch.randn(6, device="cuda", generator=g), big * torch.randn(6, device="cuda", generator=g)
+        norm, ent = fp32_norm(x, mask, scale)
+        got = xrl.xrl_logprob_grad(x, norm, token, d, ent, e, mask=mask, scale=scale)
+        assert bool((got[:, 7] == 0).all()) and bool((got[mask == 0] == 0).all()) and not bool(torch.isnan(got).any())
+        want, tol = reference_grad(x, token, mask, scale, norm, ent, d, e)
+        fits = want.abs() < torch.finfo(x.dtype).max / 2
+        near(got[fits], want[fits], tol[fits], "gradient")
+    d[0], e[1] = INF, INF
+    got = xrl.xrl_logprob_grad(x, norm, token, d, ent, e, mask=mask, scale=scale)
+    assert bool((got[mask == 0] == 0).all())
+
+
 def test_gradient_against_differences():
     """(f(x + h e_j) - f(x - h e_j)) / 2h of f = sum(dlogp logp + dentropy H) in 64 bits; its error is h^2 f''' / 6 < 1e-7
     for slopes of order one at h = 1e-4, and the fp32 gradient's own 1e-6."""
@@ -260,6 +304,22 @@ def test_gradient_against_differences():
         e[:, j] = 1e-4
         slope = (f(x.double() + e) - f(x.double() - e)) / 2e-4
         assert float((slope - got[:, j]).abs().max()) < 2e-6
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows,vocab", [(1, 60000), (200, 60000), (3, 2500)])
+@pytest.mark.parametrize("top", [1, 8, 32])
+def test_alternatives_of_every_kind_of_row(dtype, rows, vocab, top):
+    """Few distinct values, one block of large ones, rising and falling rows, few valid entries, all equal."""
+    g = torch.Generator(device="cuda").manual_seed(top)
+    at = torch.arange(vocab, device="cuda")
+    kinds = [torch.randint(0, 3, (vocab,), device="cuda", generator=g).float(), (at // 1000 == 1).float() * 5 + at * 1e-4, at * 1e-3,
+             -at * 1e-3, torch.where(torch.rand(vocab, device="cuda", generator=g) < 20 / vocab, 1.0, -INF), torch.zeros(vocab, device="cuda"),
+             torch.where(at % 512 == 3, 2.0, -1.0), torch.full((vocab,), -INF, device="cuda")]
+    x = torch.stack([kinds[i % len(kinds)] for i in range(max(rows, len(kinds)))]).to(DTYPES[dtype])
+    for first in range(0, len(x), rows):
+        part = x[first:first + rows]
+        check_scores(xrl.xrl_logprob(part, top=top), part, None, None, 1.0, top)
 
 
 def test_offsets_past_32_bits():
