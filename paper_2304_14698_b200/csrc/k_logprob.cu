@@ -98,17 +98,27 @@ __device__ __forceinline__ Sums join(const Sums& a, const Sums& b) {
   o.t = fmaf(da, a.s, a.t) * ea + fmaf(db, b.s, b.t) * eb;
   return o;
 }
-__device__ __forceinline__ Sums join_warp(Sums v) {
+__device__ __forceinline__ uint32_t key_of(float v) {          // unsigned order = order of the floats
+  const uint32_t b = __float_as_uint(v + 0.f);
+  return b & 0x80000000u ? ~b : b | 0x80000000u;
+}
+__device__ __forceinline__ float float_of(uint32_t key) {
+  return __uint_as_float(key & 0x80000000u ? key & 0x7FFFFFFFu : ~key);
+}
+__device__ __forceinline__ float max_warp(float v) { return float_of(__reduce_max_sync(kAll, key_of(v))); }      // no NaN
+__device__ __forceinline__ Sums join_warp(const Sums& v) {
+  Sums o;
+  o.m = max_warp(v.m);
+  o.r = max_warp(v.r);
+  const float d = v.r - o.r, e = ex2(d);
+  o.s = v.s * e;
+  o.t = fmaf(d, v.s, v.t) * e;
 #pragma unroll
-  for (int d = 16; d > 0; d >>= 1) {
-    Sums o;
-    o.m = __shfl_xor_sync(kAll, v.m, d);
-    o.r = __shfl_xor_sync(kAll, v.r, d);
-    o.s = __shfl_xor_sync(kAll, v.s, d);
-    o.t = __shfl_xor_sync(kAll, v.t, d);
-    v = join(v, o);
+  for (int d2 = 16; d2 > 0; d2 >>= 1) {
+    o.s += __shfl_xor_sync(kAll, o.s, d2);
+    o.t += __shfl_xor_sync(kAll, o.t, d2);
   }
-  return v;
+  return o;
 }
 
 // ---- the best k of a set, one per lane, best first; ties go to the lower index ---------------------------------
@@ -157,22 +167,27 @@ __device__ __forceinline__ float entropy_of(const Sums& v) {
 __device__ __forceinline__ float logp_of(float x, const RowNorm& n, float scale) {
   return x > kNegInf || x != x ? fmaf(scale, x - n.m, -n.l) : kNegInf;
 }
-template <typename T>
-__device__ __forceinline__ void write_row(const RowArgs& a, const RowOut& o, int64_t row, const RowNorm& n, float entropy) {
+// The row's token and its logit, asked for before the row is walked
+struct Given {
+  int32_t t = -1;
+  float x = kNegInf;
+};
+template <typename T> __device__ __forceinline__ Given given_of(const RowArgs& a, int64_t row) {
+  Given g;
+  if (a.token) {
+    g.t = __ldg(a.token + row);
+    if (g.t >= 0 && g.t < a.vocab) {
+      g.x = load1(static_cast<const T*>(a.x) + row * a.x_stride + g.t);
+      if (a.mask && !__ldg(a.mask + row * a.mask_stride + g.t)) g.x = kNegInf;
+    }
+  }
+  return g;
+}
+__device__ __forceinline__ void write_row(const RowArgs& a, const RowOut& o, int64_t row, const Given& g, const RowNorm& n,
+                                          float entropy) {
   if (o.norm) *reinterpret_cast<float2*>(o.norm + 2 * row) = make_float2(n.m, n.l);
   if (o.entropy) o.entropy[row] = entropy;
-  if (o.logp) {
-    const int32_t t = a.token[row];
-    float lp = 0.f;
-    if (t < -1 || t >= a.vocab) {
-      lp = NAN;
-    } else if (t >= 0) {
-      float x = load1(static_cast<const T*>(a.x) + row * a.x_stride + t);
-      if (a.mask && !a.mask[row * a.mask_stride + t]) x = kNegInf;
-      lp = logp_of(x, n, a.scale);
-    }
-    o.logp[row] = lp;
-  }
+  if (o.logp) o.logp[row] = g.t == -1 ? 0.f : g.t < -1 || g.t >= a.vocab ? NAN : logp_of(g.x, n, a.scale);
 }
 __device__ __forceinline__ void write_top(const RowArgs& a, const RowOut& o, int64_t row, const RowNorm& n, const Best& b,
                                           int lane) {
@@ -191,6 +206,8 @@ __global__ void __launch_bounds__(128) k_logprob_warp(RowArgs a, RowOut o) {
   const float c = a.scale * kLog2e;
   for (int64_t row = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 5); row < a.rows; row += int64_t(gridDim.x) * 4) {
     const T* x = static_cast<const T*>(a.x) + row * a.x_stride;
+    Given given;
+    if (lane == 0) given = given_of<T>(a, row);
     float v[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) {
@@ -218,7 +235,7 @@ __global__ void __launch_bounds__(128) k_logprob_warp(RowArgs a, RowOut o) {
     }
     const bool empty = q.s == 0.f;
     const RowNorm n = {m, empty ? kNegInf : kLn2 * log2f(q.s)};
-    if (lane == 0) write_row<T>(a, o, row, n, empty ? 0.f : entropy_of(q));
+    if (lane == 0) write_row(a, o, row, given, n, empty ? 0.f : entropy_of(q));
     if (o.top) {
       Best mine, last;
 #pragma unroll
@@ -267,6 +284,54 @@ __device__ __forceinline__ void mask_words(const uint8_t* p, uint32_t& m0, uint3
   m1 = 0;
   if (N == 8) m1 = __funnelshift_r(w1, off ? __ldg(w + 2) : 0u, off);
 }
+// ---- a thread's own copies ahead: what it will read, on its way to its own places in shared memory ------------------
+// Registers for two chunks and four warps a scheduler do not go together, and without loads in flight during the
+// arithmetic the rows come at half of HBM's rate (8,192 x 32,000 bf16 156 us).  cp.async needs neither registers nor, as no
+// thread reads another's places, barriers.
+template <int BYTES> __device__ __forceinline__ void copy_ahead(uint32_t dst, const void* src) {
+  if (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+  else asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copies_end_group() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+// DEPTH groups of U vectors per thread, each with the words of its mask
+template <typename T, int THREADS, int U, bool MASK> struct Ahead {
+  static constexpr int DEPTH = 3, N = Vec<T>::N, WORDS = MASK ? N / 4 + 1 : 0;
+  static constexpr int VEC_BYTES = THREADS * 16, WORD_BYTES = THREADS * 4;
+  static constexpr int GROUP_BYTES = U * (VEC_BYTES + WORDS * WORD_BYTES);
+  static constexpr int BYTES = DEPTH * GROUP_BYTES;
+  uint32_t base;                         // of the thread
+  __device__ __forceinline__ explicit Ahead(const void* smem)
+      : base(static_cast<uint32_t>(__cvta_generic_to_shared(smem)) + threadIdx.x * 16) {}
+  __device__ __forceinline__ uint32_t vec_at(int group, int u) const { return base + group * GROUP_BYTES + u * VEC_BYTES; }
+  __device__ __forceinline__ uint32_t word_at(int group, int u, int w) const {
+    return base - threadIdx.x * 12 + group * GROUP_BYTES + U * VEC_BYTES + (u * WORDS + w) * WORD_BYTES;
+  }
+  __device__ __forceinline__ void ask(int group, int u, const T* x, const uint8_t* mask) const {
+    copy_ahead<16>(vec_at(group, u), x);
+    if (MASK) {
+      const uintptr_t at = reinterpret_cast<uintptr_t>(mask);
+      const uint32_t* w = reinterpret_cast<const uint32_t*>(at & ~uintptr_t(3));
+#pragma unroll
+      for (int i = 0; i < WORDS; ++i)
+        if (i + 1 < WORDS || (at & 3)) copy_ahead<4>(word_at(group, u, i), w + i);
+    }
+  }
+  __device__ __forceinline__ uint4 take(int group, int u, const uint8_t* mask) const {
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(vec_at(group, u)) : "memory");
+    if (MASK) {
+      const uint32_t off = uint32_t(reinterpret_cast<uintptr_t>(mask) & 3) * 8;
+      uint32_t w[3] = {0u, 0u, 0u};
+#pragma unroll
+      for (int i = 0; i < WORDS; ++i)
+        asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w[i]) : "r"(word_at(group, u, i)) : "memory");
+      // (the last word is another call's where nothing was asked for; no bit of it is used then)
+      Vec<T>::drop(v, __funnelshift_r(w[0], w[1], off), N == 8 ? __funnelshift_r(w[1], w[2], off) : 0u);
+    }
+    return v;
+  }
+};
 __device__ __forceinline__ uint4 load_stream(const void* p) {
   uint4 v;
   asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
@@ -307,14 +372,6 @@ template <typename T> struct Row {
     return v;
   }
 };
-__device__ __forceinline__ uint32_t key_of(float v) {          // unsigned order = order of the floats
-  const uint32_t b = __float_as_uint(v + 0.f);
-  return b & 0x80000000u ? ~b : b | 0x80000000u;
-}
-__device__ __forceinline__ float float_of(uint32_t key) {
-  return __uint_as_float(key & 0x80000000u ? key & 0x7FFFFFFFu : ~key);
-}
-
 // A row whose logits are too far from 0 for the above: largest first, then the sums of differences.
 template <typename T, int THREADS>
 __device__ __noinline__ void careful_row(const RowArgs& a, bool masked, int64_t row, float* red, Sums& out) {
@@ -531,31 +588,98 @@ __device__ __forceinline__ void best_of_part(const Row<T>& r, int v0, int v1, bo
   rank_candidates<THREADS>(s, n, k);
 }
 
-template <typename T, int THREADS, bool MASK, bool TOP>
-__global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_logprob_cta(RowArgs a, RowOut o, int parts) {
+// A CTA takes rows first, first + step, ... (parts > 1: a cluster takes one row, each CTA a part of it).
+template <typename T, int THREADS, int U, bool MASK, bool TOP>
+__global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_logprob_cta(RowArgs a, RowOut o, int log_parts) {
+  using A = Ahead<T, THREADS, U, MASK>;
   enter();
-  constexpr int U = 4, W = THREADS / 32;
-  __shared__ Sums s_sums[W];
+  constexpr int N = Vec<T>::N, W = THREADS / 32;
+  extern __shared__ __align__(16) uint8_t s_ahead[];
+  __shared__ Sums s_sums[2][W];          // of this row and of the one before, which a warp may still read
   __shared__ float s_red[64];
   __shared__ Candidates<TOP ? THREADS : 32> s_best;
   __shared__ Sums s_part;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int64_t row = int64_t(blockIdx.x) / parts;
-  const int part = parts > 1 ? int(cluster_rank()) : 0;
-  const Row<T> r(a, row, MASK);
+  const int parts = 1 << log_parts, part = parts > 1 ? int(cluster_rank()) : 0;
+  const int64_t step = parts > 1 ? a.rows : int64_t(gridDim.x);
+  // part p of a row's vectors starts here (below 2^29 vectors and 8 parts: 32 bits)
+  auto start_of = [&](int vecs, int p) { return int((uint32_t(vecs) * uint32_t(p)) >> log_parts); };
   const float c = a.scale * kLog2e;
-  const int v0 = int(int64_t(r.vecs) * part / parts), v1 = int(int64_t(r.vecs) * (part + 1) / parts);
   // (as a bf16 number, which it is for both types; rounded, it is within 2^-9 of itself)
   const float floor = to_float(bf16(kLowest / c));
   const Sums zero = {kNegInf, floor * c, 0.f, 0.f};
+  const A ahead(s_ahead);
 
-  Sums q = zero;
-  for (int j = v0 + threadIdx.x; j < v1; j += U * THREADS) {
-    uint4 v[U];
+  // what is asked for next: of row p_row, from p_x and p_mask on (the thread's own vector), the p_left vectors that are left
+  constexpr int GROUP = U * THREADS;
+  int64_t p_row = blockIdx.x >> log_parts;
+  int p_group = 0, p_left = 0;
+  const T* p_x = nullptr;
+  const uint8_t* p_mask = nullptr;
+  auto p_start = [&]() {
+    p_left = 0;
+    if (p_row >= a.rows) return;
+    const Row<T> r(a, p_row, MASK);
+    const int v0 = start_of(r.vecs, part);
+    p_left = start_of(r.vecs, part + 1) - v0;
+    const int64_t at = r.head + (int64_t(v0) + threadIdx.x) * N;
+    p_x = r.x + at;
+    if (MASK) p_mask = r.mask + at;
+  };
+  auto ask = [&]() {                     // one group (an empty one where a row has no whole vectors, or behind the last row)
+    if (p_left >= GROUP) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) v[u] = j + u * THREADS < v1 ? r.template vec<MASK>(j + u * THREADS) : Vec<T>::none();
-    add_chunk<T, U>(q, v, c, floor);
-  }
+      for (int u = 0; u < U; ++u) ahead.ask(p_group, u, p_x + u * THREADS * N, p_mask + u * THREADS * N);
+    } else {
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (u * THREADS + int(threadIdx.x) < p_left) ahead.ask(p_group, u, p_x + u * THREADS * N, p_mask + u * THREADS * N);
+    }
+    copies_end_group();
+    p_group = p_group + 1 < A::DEPTH ? p_group + 1 : 0;
+    p_x += GROUP * N;
+    if (MASK) p_mask += GROUP * N;
+    p_left -= GROUP;
+    if (p_left <= 0) {
+      p_row += step;
+      p_start();
+    }
+  };
+  int64_t row = p_row;
+  p_start();
+#pragma unroll
+  for (int d = 0; d < A::DEPTH - 1; ++d) ask();
+
+  int group = 0, turn = 0;
+  for (; row < a.rows; row += step, turn ^= 1) {
+  const Row<T> r(a, row, MASK);
+  Given given;
+  if (threadIdx.x == 0 && part == 0) given = given_of<T>(a, row);
+  const int v0 = start_of(r.vecs, part), v1 = start_of(r.vecs, part + 1);
+  const uint8_t* mask = MASK ? r.mask + r.head + (int64_t(v0) + threadIdx.x) * N : nullptr;
+  Sums q = zero;
+  int left = v1 - v0;
+  do {
+    ask();                               // into the group taken last
+    copies_wait<A::DEPTH - 1>();
+    if (left >= GROUP) {
+      uint4 v[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) v[u] = ahead.take(group, u, mask + u * THREADS * N);
+      add_chunk<T, U>(q, v, c, floor);
+    } else if (warp * 32 < left) {       // the warp has vectors here
+#pragma unroll 1
+      for (int u = 0; u < U; ++u) {
+        const int at = u * THREADS + int(threadIdx.x);
+        if (at - lane >= left) break;
+        const uint4 v[1] = {at < left ? ahead.take(group, u, mask + u * THREADS * N) : Vec<T>::none()};
+        add_chunk<T, 1>(q, v, c, floor);
+      }
+    }
+    group = group + 1 < A::DEPTH ? group + 1 : 0;
+    if (MASK) mask += GROUP * N;
+    left -= GROUP;
+  } while (left > 0);
   const float thread_max = q.m;          // (of its whole vectors)
   if (part == 0 && threadIdx.x < 16) {
     const int j = r.edge(threadIdx.x);
@@ -565,12 +689,12 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_logprob_cta(RowArgs
     }
   }
   q = join_warp(q);
-  if (lane == 0) s_sums[warp] = q;
+  if (lane == 0) s_sums[turn][warp] = q;
   __syncthreads();
-  q = lane < W ? s_sums[lane] : zero;
-  q = join_warp(q);
-
-  if (TOP) best_of_part<T, TOP ? THREADS : 32, MASK>(r, v0, v1, part == 0, thread_max, q.m, o.top, s_best, reinterpret_cast<uint32_t*>(s_red));
+  q = lane < W ? s_sums[turn][lane] : zero;
+  float largest = max_warp(q.m);
+  if (TOP) best_of_part<T, TOP ? THREADS : 32, MASK>(r, v0, v1, part == 0, thread_max, largest, o.top, s_best, reinterpret_cast<uint32_t*>(s_red));
+  if (parts > 1 || warp == 0) q = join_warp(q);
   if (parts > 1) {
     if (threadIdx.x == 0) s_part = q;
     cluster_arrive_wait();
@@ -581,6 +705,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_logprob_cta(RowArgs
       } else if (lane >= parts) {
         q = zero;
       }
+      largest = max_warp(q.m);
       q = join_warp(q);
       if (TOP) {
         const int p = threadIdx.x / kMostTop, e = threadIdx.x % kMostTop;
@@ -595,26 +720,31 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_logprob_cta(RowArgs
       }
     }
     cluster_arrive_wait();               // nobody leaves, and nothing is written again, while it is read
-    if (part != 0) return;
+    if (part != 0) break;
     if (TOP) rank_candidates(s_best, parts * kMostTop, o.top);
   }
-  RowNorm n;
-  float entropy;
-  if (q.m > kNegInf && q.m < INFINITY && !(q.m * c > kLow && q.m * c < kHigh)) {
-    Sums z;
-    careful_row<T, THREADS>(a, MASK, row, s_red, z);
-    n = {z.m, kLn2 * log2f(z.s)};
-    entropy = entropy_of(z);
-  } else if (q.m > kNegInf || q.s != q.s) {
-    n = norm_of(q, c);
-    if (q.s != q.s) n.l = NAN;
-    entropy = entropy_of(q);
-  } else {
-    n = {kNegInf, kNegInf};
-    entropy = 0.f;
+  if (largest > kNegInf && largest < INFINITY && !(largest * c > kLow && largest * c < kHigh)) {       // (all threads agree)
+    careful_row<T, THREADS>(a, MASK, row, s_red, q);
+    if (warp == 0) {
+      const RowNorm n = {q.m, kLn2 * log2f(q.s)};
+      if (lane == 0) write_row(a, o, row, given, n, entropy_of(q));
+      if (TOP) write_top(a, o, row, n, Best{s_best.best_v[lane], s_best.best_i[lane]}, lane);
+    }
+    __syncthreads();
+  } else if (warp == 0) {
+    RowNorm n = {kNegInf, kNegInf};
+    float entropy = 0.f;
+    if (largest > kNegInf || q.s != q.s) {
+      n = norm_of(q, c);
+      if (q.s != q.s) n.l = NAN;
+      entropy = entropy_of(q);
+    }
+    if (lane == 0) write_row(a, o, row, given, n, entropy);
+    if (TOP) write_top(a, o, row, n, Best{s_best.best_v[lane], s_best.best_i[lane]}, lane);
   }
-  if (threadIdx.x == 0) write_row<T>(a, o, row, n, entropy);
-  if (TOP && warp == 0) write_top(a, o, row, n, Best{s_best.best_v[lane], s_best.best_i[lane]}, lane);
+  if (TOP) __syncthreads();              // the next row's use of the candidates
+  }
+  copies_wait<0>();
 }
 
 // ---- gradient ---------------------------------------------------------------------------------------------------
@@ -623,11 +753,45 @@ struct GradArgs {
   void* grad;
   int64_t grad_stride;
 };
-// One entry as the formula says it; what the fast form below leaves out
+// What a row's entries share, as it lies in memory and as it is used.  With p = 2^y, y = (x - m) c - l2, an entry is
+// p (A + B y), plus dl at the token: A = -(dl + dh H), B = -dh ln 2.  -infinity becomes kFloor first, for which p is 0; rows
+// where that does not do (a norm or gradients that are not finite, logits all below the floor) go entry by entry.
+struct RowInputs {
+  float2 norm = {0.f, 0.f};
+  int32_t t = -1;
+  float dlogp = 0.f, dentropy = 0.f, entropy = 0.f;
+};
+__device__ __forceinline__ RowInputs inputs_of(const RowArgs& a, const GradArgs& g, int64_t row) {
+  RowInputs r;
+  r.norm = __ldg(reinterpret_cast<const float2*>(g.norm) + row);
+  if (a.token) r.t = __ldg(a.token + row);
+  if (g.dlogp) r.dlogp = __ldg(g.dlogp + row);
+  if (g.dentropy) { r.dentropy = __ldg(g.dentropy + row); r.entropy = __ldg(g.entropy + row); }
+  return r;
+}
 struct RowGrad {
-  float m, c, l2, dl, dh, ent;           // l2: l in powers of two; dl, dh times the scale
+  float m, c, l2, dl, dh, ent, A, B;     // l2: l in powers of two; dl, dh times the scale
   int32_t t;
+  bool fast;
+  __device__ __forceinline__ RowGrad(const RowArgs& a, const RowInputs& r) {
+    t = r.t;
+    m = r.norm.x;
+    c = a.scale * kLog2e;
+    l2 = r.norm.y * kLog2e;
+    dl = t == -1 ? 0.f : t < -1 || t >= a.vocab ? NAN : a.scale * r.dlogp;
+    dh = a.scale * r.dentropy;
+    ent = r.entropy;
+    A = -fmaf(dh, ent, dl);
+    B = -dh * kLn2;
+    // (every product of the fast form is finite then)
+    fast = m > kFloor && fabsf(A) + fabsf(B) * fmaf(fabsf(m) - kFloor, c, fabsf(l2)) < INFINITY;
+  }
+  // one entry; of a fast row with the roundings of a whole vector
   __device__ __forceinline__ float operator()(float x, int j) const {
+    if (fast) {
+      const float y = fmaf(max_nan(x, kFloor) - m, c, -l2), d = ex2(y) * fmaf(y, B, A);
+      return j == t && x > kNegInf ? d + dl : d;
+    }
     const float y = fmaf(x - m, c, -l2), p = ex2(y);
     const float g = fmaf(dl, (j == t ? 1.f : 0.f) - p, p > 0.f || p != p ? -dh * p * fmaf(kLn2, y, ent) : 0.f);
     return x > kNegInf || x != x ? g : 0.f;
@@ -646,13 +810,62 @@ template <> __device__ __forceinline__ uint4 round_pairs<float>(const f32x2* g) 
   for (int i = 0; i < 2; ++i) unpair(g[i], f[2 * i], f[2 * i + 1]);
   return pack(f);
 }
-// A warp takes 32 x U vectors of a row at a time.  With p = 2^y the entry is p (A + B y), plus dl at the token:
-// A = -(dl + dh H), B = -dh ln 2.  -infinity becomes kFloor first, for which p is 0; rows where that does not do (a norm
-// or gradients that are not finite, logits all below the floor) go entry by entry.
+// the gradient of a vector's entries j ... j + N - 1
+template <typename T>
+__device__ __forceinline__ void grad_vector(const RowGrad& f, const uint4& v, int j, T* out, bool whole) {
+  constexpr int N = Vec<T>::N, P = N / 2;
+  uint4 w;
+  if (f.fast) {
+    const f32x2 mm = pair(-f.m, -f.m), cc = pair(f.c, f.c), ll = pair(-f.l2, -f.l2), aa = pair(f.A, f.A), bb = pair(f.B, f.B);
+    f32x2 x[P];
+    const uint4 one[1] = {v};
+    spread<1>(one, x, kFloor, static_cast<const T*>(nullptr));
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+      const f32x2 y = fma2(add2(x[i], mm), cc, ll);
+      float y0, y1;
+      unpair(y, y0, y1);
+      x[i] = mul2(pair(ex2(y0), ex2(y1)), fma2(y, bb, aa));
+    }
+    if (uint32_t(f.t - j) < uint32_t(N)) {               // (a token outside the support has no share)
+      float z[N];
+      unpack(v, z);
+#pragma unroll
+      for (int i = 0; i < P; ++i) {
+        float lo, hi;
+        unpair(x[i], lo, hi);
+        x[i] = pair(f.t - j == 2 * i && z[2 * i] > kNegInf ? lo + f.dl : lo,
+                    f.t - j == 2 * i + 1 && z[2 * i + 1] > kNegInf ? hi + f.dl : hi);
+      }
+    }
+    w = round_pairs<T>(x);
+  } else {
+    float z[N];
+    unpack(v, z);
+#pragma unroll
+    for (int i = 0; i < N; ++i) z[i] = f(z[i], j + i);
+    w = pack(z);
+  }
+  if (whole) {
+    *reinterpret_cast<uint4*>(out + j) = w;
+  } else {
+    const T* e = reinterpret_cast<const T*>(&w);
+#pragma unroll
+    for (int i = 0; i < N; ++i) out[j + i] = e[i];
+  }
+}
+template <typename T>
+__device__ __forceinline__ void grad_edges(const RowGrad& f, const Row<T>& r, T* out, int i) {
+  const int j = i < 16 ? r.edge(i) : -1;
+  if (j >= 0) out[j] = T(f(r.at(j), j));
+}
+template <typename T> __device__ __forceinline__ bool aligned16(const T* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+// Short rows: a warp takes 32 x U vectors of a row at a time.
 template <typename T, bool MASK>
 __global__ void __launch_bounds__(256) k_logprob_grad(RowArgs a, GradArgs g, int segs) {
   enter();
-  constexpr int N = Vec<T>::N, U = 4, P = N / 2;
+  constexpr int N = Vec<T>::N, U = 4;
   const int lane = threadIdx.x & 31;
   const int64_t items = a.rows * segs, step = int64_t(gridDim.x) * 8;
   for (int64_t item = int64_t(blockIdx.x) * 8 + (threadIdx.x >> 5); item < items; item += step) {
@@ -664,87 +877,110 @@ __global__ void __launch_bounds__(256) k_logprob_grad(RowArgs a, GradArgs g, int
 #pragma unroll
     for (int u = 0; u < U; ++u) v[u] = j0 + u * 32 < r.vecs ? r.template vec<MASK>(j0 + u * 32) : Vec<T>::none();
     T* out = static_cast<T*>(g.grad) + row * g.grad_stride;
-    RowGrad f;
-    const float2 n = __ldg(reinterpret_cast<const float2*>(g.norm) + row);
-    f.t = a.token ? __ldg(a.token + row) : -1;
-    f.m = n.x;
-    f.c = a.scale * kLog2e;
-    f.l2 = n.y * kLog2e;
-    f.dl = f.t == -1 || !g.dlogp ? 0.f : f.t < -1 || f.t >= a.vocab ? NAN : a.scale * __ldg(g.dlogp + row);
-    f.dh = g.dentropy ? a.scale * __ldg(g.dentropy + row) : 0.f;
-    f.ent = g.dentropy ? __ldg(g.entropy + row) : 0.f;
-    const bool whole = ((reinterpret_cast<uintptr_t>(out + r.head)) & 15) == 0;
-    const float A = -fmaf(f.dh, f.ent, f.dl), B = -f.dh * kLn2;
-    // (every product of the fast form is finite then)
-    const bool fast = f.m > kFloor && fabsf(A) + fabsf(B) * fmaf(fabsf(f.m) - kFloor, f.c, fabsf(f.l2)) < INFINITY;
-    if (fast) {
-      const f32x2 mm = pair(-f.m, -f.m), cc = pair(f.c, f.c), ll = pair(-f.l2, -f.l2), aa = pair(A, A), bb = pair(B, B);
+    const RowGrad f(a, inputs_of(a, g, row));
+    const bool whole = aligned16(out + r.head);
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        if (j0 + u * 32 >= r.vecs) break;
-        const int j = r.head + (j0 + u * 32) * N;
-        f32x2 x[P];
-        const uint4 one[1] = {v[u]};
-        spread<1>(one, x, kFloor, static_cast<const T*>(nullptr));
-#pragma unroll
-        for (int i = 0; i < P; ++i) {
-          const f32x2 y = fma2(add2(x[i], mm), cc, ll);
-          float y0, y1;
-          unpair(y, y0, y1);
-          x[i] = mul2(pair(ex2(y0), ex2(y1)), fma2(y, bb, aa));
-        }
-        if (uint32_t(f.t - j) < uint32_t(N)) {           // (a token outside the support has no share)
-          float z[N];
-          unpack(v[u], z);
-          bool kept = false;
-#pragma unroll
-          for (int i = 0; i < N; ++i) kept |= f.t - j == i && z[i] > kNegInf;
-#pragma unroll
-          for (int i = 0; i < P; ++i) {
-            float lo, hi;
-            unpair(x[i], lo, hi);
-            x[i] = pair(f.t - j == 2 * i && kept ? lo + f.dl : lo, f.t - j == 2 * i + 1 && kept ? hi + f.dl : hi);
-          }
-        }
-        const uint4 w = round_pairs<T>(x);
-        if (whole) {
-          *reinterpret_cast<uint4*>(out + j) = w;
-        } else {
-          const T* e = reinterpret_cast<const T*>(&w);
-#pragma unroll
-          for (int i = 0; i < N; ++i) out[j + i] = e[i];
-        }
-      }
-    } else {
-#pragma unroll 1
-      for (int u = 0; u < U; ++u) {
-        if (j0 + u * 32 >= r.vecs) break;
-        const int j = r.head + (j0 + u * 32) * N;
-        float x[N];
-        unpack(r.template vec<MASK>(j0 + u * 32), x);
-#pragma unroll
-        for (int i = 0; i < N; ++i) out[j + i] = T(f(x[i], j + i));
-      }
-    }
-    if (seg == 0 && lane < 16) {
-      const int j = r.edge(lane);
-      if (j >= 0) {
-        const float x = r.at(j);
-        float d = f(x, j);
-        if (fast) {                      // the same roundings as in a whole vector
-          const float y = fmaf(max_nan(x, kFloor) - f.m, f.c, -f.l2);
-          d = ex2(y) * fmaf(y, B, A);
-          if (j == f.t && x > kNegInf) d += f.dl;
-        }
-        out[j] = T(d);
-      }
-    }
+    for (int u = 0; u < U; ++u)
+      if (j0 + u * 32 < r.vecs) grad_vector(f, v[u], r.head + (j0 + u * 32) * N, out, whole);
+    if (seg == 0) grad_edges(f, r, out, lane);
   }
 }
 
+// Long rows: resident CTAs take pieces of rows in turn, each `piece` vectors, copied ahead across pieces; what a row shares
+// is asked for a piece ahead too.
+template <typename T, int THREADS, int U, bool MASK>
+__global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_logprob_grad_rows(RowArgs a, GradArgs g, int pieces, int piece) {
+  using A = Ahead<T, THREADS, U, MASK>;
+  enter();
+  constexpr int N = Vec<T>::N, GROUP = U * THREADS;
+  extern __shared__ __align__(16) uint8_t s_ahead[];
+  const A ahead(s_ahead);
+  const int64_t units = a.rows * pieces;
+  auto split = [&](int64_t unit, int64_t& row, int& at) {
+    row = units <= INT32_MAX ? int64_t(uint32_t(unit) / uint32_t(pieces)) : unit / pieces;
+    at = int(unit - row * pieces) * piece;
+  };
+  int64_t p_unit = blockIdx.x;
+  int p_group = 0, p_left = 0;
+  const T* p_x = nullptr;
+  const uint8_t* p_mask = nullptr;
+  auto p_start = [&]() {
+    p_left = 0;
+    if (p_unit >= units) return;
+    int64_t row;
+    int v0;
+    split(p_unit, row, v0);
+    const Row<T> r(a, row, MASK);
+    p_left = min(r.vecs - v0, piece);
+    const int64_t at = r.head + (int64_t(v0) + threadIdx.x) * N;
+    p_x = r.x + at;
+    if (MASK) p_mask = r.mask + at;
+  };
+  auto ask = [&]() {
+    if (p_left >= GROUP) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) ahead.ask(p_group, u, p_x + u * THREADS * N, p_mask + u * THREADS * N);
+    } else {
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (u * THREADS + int(threadIdx.x) < p_left) ahead.ask(p_group, u, p_x + u * THREADS * N, p_mask + u * THREADS * N);
+    }
+    copies_end_group();
+    p_group = p_group + 1 < A::DEPTH ? p_group + 1 : 0;
+    p_x += GROUP * N;
+    if (MASK) p_mask += GROUP * N;
+    p_left -= GROUP;
+    if (p_left <= 0) {
+      p_unit += gridDim.x;
+      p_start();
+    }
+  };
+  p_start();
+#pragma unroll
+  for (int d = 0; d < A::DEPTH - 1; ++d) ask();
+  int group = 0;
+  RowInputs next;
+  int64_t row = 0;
+  int v0 = 0;
+  if (int64_t(blockIdx.x) < units) {
+    split(blockIdx.x, row, v0);
+    next = inputs_of(a, g, row);
+  }
+  for (int64_t unit = blockIdx.x; unit < units; unit += gridDim.x) {
+    const RowGrad f(a, next);
+    split(unit, row, v0);
+    const Row<T> r(a, row, MASK);
+    T* out = static_cast<T*>(g.grad) + row * g.grad_stride;
+    const bool whole = aligned16(out + r.head);
+    if (unit + gridDim.x < units) {
+      int64_t then;
+      int at;
+      split(unit + gridDim.x, then, at);
+      next = inputs_of(a, g, then);
+    }
+    if (v0 == 0) grad_edges(f, r, out, threadIdx.x);
+    int left = min(r.vecs - v0, piece), j = r.head + (v0 + int(threadIdx.x)) * N;
+    const uint8_t* mask = MASK ? r.mask + j : nullptr;
+    do {
+      ask();
+      copies_wait<A::DEPTH - 1>();
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (u * THREADS + int(threadIdx.x) < left)
+          grad_vector(f, ahead.take(group, u, mask + u * THREADS * N), j + u * THREADS * N, out, whole);
+      group = group + 1 < A::DEPTH ? group + 1 : 0;
+      j += GROUP * N;
+      if (MASK) mask += GROUP * N;
+      left -= GROUP;
+    } while (left > 0);
+  }
+  copies_wait<0>();
+}
+
 template <typename K, typename... A>
-void launch_cluster(K kernel, unsigned grid, unsigned threads, unsigned cluster, cudaStream_t st, A... args) {
+void launch_cluster(K kernel, unsigned grid, unsigned threads, size_t smem, unsigned cluster, cudaStream_t st, A... args) {
   cudaLaunchConfig_t cfg = {};
+  cfg.dynamicSmemBytes = smem;
   cfg.gridDim = grid;
   cfg.blockDim = threads;
   cfg.stream = st;
@@ -759,61 +995,80 @@ void launch_cluster(K kernel, unsigned grid, unsigned threads, unsigned cluster,
   cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
-#ifndef LP_THREADS
-#define LP_THREADS 512
-#endif
-constexpr int kThreads = LP_THREADS;
-template <typename T, bool MASK, int THREADS>
-void launch_cta(const RowArgs& a, const RowOut& o, int parts, cudaStream_t st) {
-  const unsigned grid = unsigned(a.rows * parts);
-  if (o.top) launch_cluster(k_logprob_cta<T, THREADS, MASK, true>, grid, THREADS, parts, st, a, o, parts);
-  else launch_cluster(k_logprob_cta<T, THREADS, MASK, false>, grid, THREADS, parts, st, a, o, parts);
+template <typename T, int THREADS, int U, bool MASK, bool TOP>
+bool launch_cta(const RowArgs& a, const RowOut& o, int parts, cudaStream_t st) {
+  constexpr int SMEM = Ahead<T, THREADS, U, MASK>::BYTES;
+  static bool done[64] = {};
+  if (!ensure_dynamic_smem(k_logprob_cta<T, THREADS, U, MASK, TOP>, SMEM, done)) return false;
+  // resident CTAs: 64 registers a thread, 227 KB of shared memory
+  constexpr int FIT = (227 * 1024) / (SMEM + 8 * 1024), MOST = 1024 / THREADS < FIT ? 1024 / THREADS : FIT;
+  const int64_t work = a.rows * parts, most = parts > 1 ? work : int64_t(kNumSMs) * MOST;
+  launch_cluster(k_logprob_cta<T, THREADS, U, MASK, TOP>, unsigned(work < most ? work : most), THREADS, SMEM, parts, st, a, o,
+                 parts == 8 ? 3 : parts == 4 ? 2 : parts == 2 ? 1 : 0);
+  return true;
 }
-template <typename T, bool MASK>
-void launch_rows(const RowArgs& a, const RowOut& o, cudaStream_t st) {
-  if (a.vocab <= 1024) {
-    const int64_t ctas = (a.rows + 3) / 4;
-    const unsigned grid = unsigned(ctas < (int64_t(1) << 30) ? ctas : int64_t(1) << 30);
-    if (a.vocab <= 128) launch(k_logprob_warp<T, 4, MASK>, grid, 128, 0, st, a, o);
-    else if (a.vocab <= 256) launch(k_logprob_warp<T, 8, MASK>, grid, 128, 0, st, a, o);
-    else if (a.vocab <= 512) launch(k_logprob_warp<T, 16, MASK>, grid, 128, 0, st, a, o);
-    else launch(k_logprob_warp<T, 32, MASK>, grid, 128, 0, st, a, o);
-    return;
-  }
+template <typename T, bool MASK, bool TOP>
+bool launch_long(const RowArgs& a, const RowOut& o, cudaStream_t st) {
+  // Few rows: a cluster of up to 8 CTAs for each, none with less than 4,096 entries; then larger CTAs; then small ones, whose
+  // rows end one by one (8,192 x 32,000 bf16: 128 threads 114 us, 256 121; with alternatives, whose search is work for a
+  // CTA, 1,500 x 50,001 fp32 masked: 128 threads 102 us, 256 89).
+  constexpr int U = MASK ? 2 : 4, FEW = TOP ? 256 : 128;
   int parts = 1;
   while (parts < 8 && a.rows * parts * 2 <= 2 * kNumSMs && a.vocab / (parts * 2) >= 4096) parts *= 2;
-  launch_cta<T, MASK, kThreads>(a, o, parts, st);
+  if (a.rows * parts <= 2 * kNumSMs) return launch_cta<T, 512, 2, MASK, TOP>(a, o, parts, st);
+  if (a.rows <= 4 * kNumSMs) return launch_cta<T, 256, U, MASK, TOP>(a, o, 1, st);
+  return launch_cta<T, FEW, U, MASK, TOP>(a, o, 1, st);
 }
 template <typename T, bool MASK>
-void launch_grad(const RowArgs& a, const GradArgs& g, cudaStream_t st) {
-  const int segs = a.vocab / Vec<T>::N / (32 * 4) + 1;
+bool launch_rows(const RowArgs& a, const RowOut& o, cudaStream_t st) {
+  if (a.vocab > 1024) return o.top ? launch_long<T, MASK, true>(a, o, st) : launch_long<T, MASK, false>(a, o, st);
+  const int64_t ctas = (a.rows + 3) / 4;
+  const unsigned grid = unsigned(ctas < (int64_t(1) << 30) ? ctas : int64_t(1) << 30);
+  if (a.vocab <= 128) launch(k_logprob_warp<T, 4, MASK>, grid, 128, 0, st, a, o);
+  else if (a.vocab <= 256) launch(k_logprob_warp<T, 8, MASK>, grid, 128, 0, st, a, o);
+  else if (a.vocab <= 512) launch(k_logprob_warp<T, 16, MASK>, grid, 128, 0, st, a, o);
+  else launch(k_logprob_warp<T, 32, MASK>, grid, 128, 0, st, a, o);
+  return true;
+}
+template <typename T, bool MASK>
+bool launch_grad(const RowArgs& a, const GradArgs& g, cudaStream_t st) {
+  constexpr int THREADS = 256, U = MASK ? 2 : 4, SMEM = Ahead<T, THREADS, U, MASK>::BYTES;
+  const int vecs = a.vocab / Vec<T>::N;
+  if (vecs >= 2 * THREADS) {             // (shorter rows leave half a group empty)
+    static bool done[64] = {};
+    if (!ensure_dynamic_smem(k_logprob_grad_rows<T, THREADS, U, MASK>, SMEM, done)) return false;
+    const int piece = 2 * U * THREADS, pieces = (vecs + piece - 1) / piece;
+    const int64_t units = a.rows * pieces, most = int64_t(kNumSMs) * (1024 / THREADS);
+    launch(k_logprob_grad_rows<T, THREADS, U, MASK>, unsigned(units < most ? units : most), THREADS, SMEM, st, a, g, pieces, piece);
+    return true;
+  }
+  const int segs = vecs / (32 * 4) + 1;
   const int64_t ctas = (a.rows * segs + 7) / 8;
   const unsigned grid = unsigned(ctas < (int64_t(1) << 30) ? ctas : int64_t(1) << 30);
   launch(k_logprob_grad<T, MASK>, grid, 256, 0, st, a, g, segs);
+  return true;
 }
 
 }  // namespace
 
-int launch_logprob(int dtype, int64_t rows, int32_t vocab, const void* logits, int64_t row_stride, const int32_t* token,
+bool launch_logprob(int dtype, int64_t rows, int32_t vocab, const void* logits, int64_t row_stride, const int32_t* token,
                    const uint8_t* mask, int64_t mask_stride, float scale, int32_t num_top, float* logp, float* entropy,
                    float* norm, int32_t* top_token, float* top_logp, cudaStream_t st) {
-  if (rows <= 0) return 0;
+  if (rows <= 0) return true;
   const RowArgs a = {logits, row_stride, token, mask, mask_stride, rows, vocab, scale};
   const RowOut o = {logp, entropy, norm, top_token, top_logp, num_top};
-  if (dtype == XRL_BF16) mask ? launch_rows<bf16, true>(a, o, st) : launch_rows<bf16, false>(a, o, st);
-  else mask ? launch_rows<float, true>(a, o, st) : launch_rows<float, false>(a, o, st);
-  return 1;
+  if (dtype == XRL_BF16) return mask ? launch_rows<bf16, true>(a, o, st) : launch_rows<bf16, false>(a, o, st);
+  return mask ? launch_rows<float, true>(a, o, st) : launch_rows<float, false>(a, o, st);
 }
 
-int launch_logprob_grad(int dtype, int64_t rows, int32_t vocab, const void* logits, int64_t row_stride, const int32_t* token,
+bool launch_logprob_grad(int dtype, int64_t rows, int32_t vocab, const void* logits, int64_t row_stride, const int32_t* token,
                         const uint8_t* mask, int64_t mask_stride, float scale, const float* norm, const float* dlogp,
                         const float* entropy, const float* dentropy, void* grad, int64_t grad_stride, cudaStream_t st) {
-  if (rows <= 0) return 0;
+  if (rows <= 0) return true;
   const RowArgs a = {logits, row_stride, token, mask, mask_stride, rows, vocab, scale};
   const GradArgs g = {norm, dlogp, entropy, dentropy, grad, grad_stride};
-  if (dtype == XRL_BF16) mask ? launch_grad<bf16, true>(a, g, st) : launch_grad<bf16, false>(a, g, st);
-  else mask ? launch_grad<float, true>(a, g, st) : launch_grad<float, false>(a, g, st);
-  return 1;
+  if (dtype == XRL_BF16) return mask ? launch_grad<bf16, true>(a, g, st) : launch_grad<bf16, false>(a, g, st);
+  return mask ? launch_grad<float, true>(a, g, st) : launch_grad<float, false>(a, g, st);
 }
 
 }  // namespace xrl

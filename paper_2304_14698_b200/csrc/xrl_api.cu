@@ -1301,10 +1301,10 @@ xrl_status xrl_logprob(int32_t device, int32_t dtype, int32_t rows, int32_t voca
     return XRL_ERR_INVALID_ARG;
   if (num_top > XRL_MAX_TOP) return XRL_ERR_UNSUPPORTED;
   XRL_ON_DEVICE(device);
-  launch_logprob(dtype, rows, vocab, logits, row_stride, token, mask, mask_stride, scale, num_top, logp, entropy, norm,
-                 top_token, top_logp, static_cast<cudaStream_t>(stream));
+  const bool done = launch_logprob(dtype, rows, vocab, logits, row_stride, token, mask, mask_stride, scale, num_top, logp, entropy,
+                                   norm, top_token, top_logp, static_cast<cudaStream_t>(stream));
   XRL_CUDA(cudaGetLastError());
-  return XRL_OK;
+  return done ? XRL_OK : XRL_ERR_CUDA;
 }
 
 xrl_status xrl_logprob_grad(int32_t device, int32_t dtype, int32_t rows, int32_t vocab, const void* logits,
@@ -1317,10 +1317,10 @@ xrl_status xrl_logprob_grad(int32_t device, int32_t dtype, int32_t rows, int32_t
       (grad && grad == logits && rows > 1 && grad_stride != row_stride))
     return XRL_ERR_INVALID_ARG;
   XRL_ON_DEVICE(device);
-  launch_logprob_grad(dtype, rows, vocab, logits, row_stride, token, mask, mask_stride, scale, norm, dlogp, entropy, dentropy,
-                      grad, grad_stride, static_cast<cudaStream_t>(stream));
+  const bool done = launch_logprob_grad(dtype, rows, vocab, logits, row_stride, token, mask, mask_stride, scale, norm, dlogp,
+                                        entropy, dentropy, grad, grad_stride, static_cast<cudaStream_t>(stream));
   XRL_CUDA(cudaGetLastError());
-  return XRL_OK;
+  return done ? XRL_OK : XRL_ERR_CUDA;
 }
 
 static xrl_status matrices_ok(int32_t dtype, int32_t batch, int32_t rows, int32_t cols) {

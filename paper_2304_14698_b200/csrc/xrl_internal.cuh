@@ -285,11 +285,12 @@ int launch_gat_layer_bwd(const Dims& d, const int32_t* rowptr, const int32_t* co
                          float* ga_dst, float* gb, int32_t N, int32_t* status, cudaStream_t st);
 int launch_gae(const float* reward, const float* values, const uint8_t* done, float gamma, float lambda, int32_t T,
                int32_t M, float* adv, float* ret, cudaStream_t st);
-// rows of logits: scoring and its gradient (see xrl_logprob, xrl_logprob_grad); token, mask, outputs may be null
-int launch_logprob(int dtype, int64_t rows, int32_t vocab, const void* logits, int64_t row_stride, const int32_t* token,
+// rows of logits: scoring and its gradient (see xrl_logprob, xrl_logprob_grad); token, mask, outputs may be null.
+// False: an attribute was refused.
+bool launch_logprob(int dtype, int64_t rows, int32_t vocab, const void* logits, int64_t row_stride, const int32_t* token,
                    const uint8_t* mask, int64_t mask_stride, float scale, int32_t num_top, float* logp, float* entropy,
                    float* norm, int32_t* top_token, float* top_logp, cudaStream_t st);
-int launch_logprob_grad(int dtype, int64_t rows, int32_t vocab, const void* logits, int64_t row_stride, const int32_t* token,
+bool launch_logprob_grad(int dtype, int64_t rows, int32_t vocab, const void* logits, int64_t row_stride, const int32_t* token,
                         const uint8_t* mask, int64_t mask_stride, float scale, const float* norm, const float* dlogp,
                         const float* entropy, const float* dentropy, void* grad, int64_t grad_stride, cudaStream_t st);
 // Newton-Schulz orthogonalisation; status: DEVICE word or null (one in the workspace).  False: a tensor map or an
