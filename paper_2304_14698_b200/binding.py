@@ -336,40 +336,53 @@ def xrl_gae(reward, values, done, gamma, lam, adv=None, ret=None, stream=None):
     return adv, ret
 
 
-def _device_of(where, *tensors):
+_torch = None
+
+
+def _th():
+    """torch, asked for when the first tensor is given (the import statement alone is 0.3 us a call)."""
+    global _torch
+    if _torch is None:
+        import torch
+        _torch = torch
+    return _torch
+
+
+def _device_of(where, first, *others):
     """The one CUDA device that all tensors (None: not given) are on."""
-    dev = next(t for t in tensors if t is not None).device
-    if dev.type != "cuda" or any(t is not None and t.device != dev for t in tensors):
-        raise XrlError(1, f"{where} (every tensor on one CUDA device)")
-    return dev.index
+    dev = first.get_device()
+    if dev < 0:
+        raise XrlError(1, f"{where} (tensors on a CUDA device)")
+    for t in others:
+        if t is not None and t.get_device() != dev:
+            raise XrlError(1, f"{where} (every tensor on one CUDA device)")
+    return dev
 
 
 def _storage(where, t):
-    name = str(t.dtype)
-    if name not in ("torch.float32", "torch.bfloat16"):
-        raise XrlError(8, f"{where} ({name}: float32 or bfloat16)")
-    return XRL_BF16 if name == "torch.bfloat16" else XRL_FP32
+    if t.dtype is _th().float32:
+        return XRL_FP32
+    if t.dtype is _th().bfloat16:
+        return XRL_BF16
+    raise XrlError(8, f"{where} ({t.dtype}: float32 or bfloat16)")
 
 
 def _stream_on(device, stream):
-    if stream is not None:
-        return C.c_void_p(int(stream))
-    import torch
-    return C.c_void_p(torch._C._cuda_getCurrentRawStream(device))
+    return _th()._C._cuda_getCurrentRawStream(device) if stream is None else int(stream)
 
 
-def _flat(where, what, t, dtype, *shape):
+def _flat(where, what, t, dtype, shape):
     """The pointer of an argument that has to be a contiguous tensor of this type and shape (or None)."""
     if t is None:
         return None
-    if str(t.dtype) != "torch." + dtype or tuple(t.shape) != shape or not t.is_contiguous():
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
         raise XrlError(1, f"{where} ({what}: contiguous {dtype} {list(shape)})")
     return t.data_ptr()
 
 
 def _rows_of(where, what, t, rows, vocab):
     """(pointer, row stride) of a [rows x vocab] tensor whose rows may lie apart."""
-    if t.dim() != 2 or tuple(t.shape) != (rows, vocab) or (vocab > 1 and t.stride(1) != 1):
+    if t.shape != (rows, vocab) or (vocab > 1 and t.stride(1) != 1):
         raise XrlError(1, f"{where} ({what}: [{rows} x {vocab}], entries of a row side by side)")
     return t.data_ptr(), t.stride(0) if rows > 1 else vocab
 
@@ -378,7 +391,7 @@ def _mask_of(where, mask, rows, vocab):
     """(pointer, row stride) of a mask: uint8 or bool, [rows x vocab] or one row for all."""
     if mask is None:
         return None, 0
-    if str(mask.dtype) not in ("torch.uint8", "torch.bool") or mask.dim() not in (1, 2):
+    if (mask.dtype is not _th().uint8 and mask.dtype is not _th().bool) or mask.dim() not in (1, 2):
         raise XrlError(1, f"{where} (mask: uint8 or bool, [rows x vocab], [1 x vocab] or [vocab])")
     one = mask.dim() == 1 or (mask.shape[0] == 1 and rows != 1)
     ptr, stride = _rows_of(where, "mask", mask if mask.dim() == 2 else mask[None], 1 if one else rows, vocab)
@@ -389,29 +402,40 @@ def xrl_logprob(logits, token=None, mask=None, scale=1.0, top=0, out=None, strea
     """Rows of logits as categorical distributions (see include/xrl.h).  logits: torch CUDA [rows, vocab], float32 or
     bfloat16, entries of a row side by side; token: int32 [rows], -1 = none; mask: uint8 or bool [rows, vocab], or one row
     for all; top: how many alternatives.  Returns a dict: entropy [rows], norm [rows, 2], with a token logp [rows], with
-    alternatives top_token and top_logp [rows, top]; out: a dict an earlier call of the same sizes returned, to be
-    written again."""
+    alternatives top_token and top_logp [rows, top]; out: a dict of the ones that are wanted, to be written in their
+    place (an earlier call's, say)."""
     where = "xrl_logprob"
-    import torch
+    th = _th()
     if logits.dim() != 2:
         raise XrlError(1, f"{where} (logits: [rows x vocab])")
     rows, vocab = logits.shape
-    o = {} if out is None else out
-    dev = _device_of(where, logits, token, mask, *o.values())
+    f32 = th.float32
     if out is None:
-        new = lambda *shape, dtype=torch.float32: torch.empty(shape, dtype=dtype, device=logits.device)  # noqa: E731
-        o = {"entropy": new(rows), "norm": new(rows, 2)}
+        dev = _device_of(where, logits, token, mask)
+        entropy = th.empty(rows, dtype=f32, device=logits.device)
+        norm = entropy.new_empty((rows, 2))
+        o = {"entropy": entropy, "norm": norm}
+        ep, np_, lp, tt, tl = entropy.data_ptr(), norm.data_ptr(), None, None, None
         if token is not None:
-            o["logp"] = new(rows)
+            o["logp"] = logp = entropy.new_empty(rows)
+            lp = logp.data_ptr()
         if top > 0:
-            o["top_token"], o["top_logp"] = new(rows, top, dtype=torch.int32), new(rows, top)
+            o["top_token"] = a = entropy.new_empty((rows, top), dtype=th.int32)
+            o["top_logp"] = b = entropy.new_empty((rows, top))
+            tt, tl = a.data_ptr(), b.data_ptr()
+    else:
+        o = out
+        dev = _device_of(where, logits, token, mask, *o.values())
+        ep = _flat(where, "entropy", o.get("entropy"), f32, (rows,))
+        np_ = _flat(where, "norm", o.get("norm"), f32, (rows, 2))
+        lp = _flat(where, "logp", o.get("logp"), f32, (rows,))
+        tt = _flat(where, "top_token", o.get("top_token"), th.int32, (rows, top))
+        tl = _flat(where, "top_logp", o.get("top_logp"), f32, (rows, top))
     x, stride = _rows_of(where, "logits", logits, rows, vocab)
     mp, mstride = _mask_of(where, mask, rows, vocab)
-    ptr = lambda name, dtype, *shape: _flat(where, name, o.get(name), dtype, *shape)  # noqa: E731
-    st = load_library().xrl_logprob(
-        dev, _storage(where, logits), rows, vocab, x, stride, _flat(where, "token", token, "int32", rows), mp, mstride, scale,
-        top, ptr("logp", "float32", rows), ptr("entropy", "float32", rows), ptr("norm", "float32", rows, 2),
-        ptr("top_token", "int32", rows, top), ptr("top_logp", "float32", rows, top), _stream_on(dev, stream))
+    st = load_library().xrl_logprob(dev, _storage(where, logits), rows, vocab, x, stride,
+                                    _flat(where, "token", token, th.int32, (rows,)), mp, mstride, scale, top, lp, ep, np_, tt, tl,
+                                    _stream_on(dev, stream))
     _check(st, where)
     return o
 
@@ -422,24 +446,25 @@ def xrl_logprob_grad(logits, norm, token=None, dlogp=None, entropy=None, dentrop
     to xrl_logprob, norm and entropy as it returned them; dlogp, dentropy: float32 [rows] or None = 0.  grad: like the logits
     and of their type, may be the logits themselves; allocated (contiguous) if None."""
     where = "xrl_logprob_grad"
-    import torch
+    th = _th()
     if logits.dim() != 2:
         raise XrlError(1, f"{where} (logits: [rows x vocab])")
     rows, vocab = logits.shape
+    f32, each = th.float32, (rows,)
     dev = _device_of(where, logits, norm, token, dlogp, entropy, dentropy, mask, grad)
-    if grad is None:
-        grad = torch.empty((rows, vocab), dtype=logits.dtype, device=logits.device)
     dtype = _storage(where, logits)
-    if grad.dtype != logits.dtype:
+    if grad is None:
+        grad = logits.new_empty((rows, vocab))
+    elif grad.dtype is not logits.dtype:
         raise XrlError(1, f"{where} (grad: the type of the logits)")
     x, stride = _rows_of(where, "logits", logits, rows, vocab)
     gp, gstride = _rows_of(where, "grad", grad, rows, vocab)
     mp, mstride = _mask_of(where, mask, rows, vocab)
-    vec = lambda name, t: _flat(where, name, t, "float32", rows)  # noqa: E731
     st = load_library().xrl_logprob_grad(
-        dev, dtype, rows, vocab, x, stride, _flat(where, "token", token, "int32", rows), mp, mstride, scale,
-        _flat(where, "norm", norm, "float32", rows, 2), vec("dlogp", dlogp), vec("entropy", entropy),
-        vec("dentropy", dentropy), gp, gstride, _stream_on(dev, stream))
+        dev, dtype, rows, vocab, x, stride, _flat(where, "token", token, th.int32, each), mp, mstride, scale,
+        _flat(where, "norm", norm, f32, (rows, 2)), _flat(where, "dlogp", dlogp, f32, each),
+        _flat(where, "entropy", entropy, f32, each), _flat(where, "dentropy", dentropy, f32, each), gp, gstride,
+        _stream_on(dev, stream))
     _check(st, where)
     return grad
 
@@ -463,7 +488,7 @@ def xrl_orthogonalise(grad, steps=5, eps=1e-7, out=None, workspace=None, device_
     (contiguous) if None; workspace: uint8 tensor of xrl_orthogonalise_workspace bytes, allocated if None (on the call's
     stream, so it is safe to let go); device_status: int32 [1] or None."""
     where = "xrl_orthogonalise"
-    import torch
+    torch = _th()
     if grad.dim() not in (2, 3):
         raise XrlError(1, f"{where} (grad: [rows x cols] or [batch x rows x cols])")
     rows, cols = grad.shape[-2:]
@@ -483,11 +508,11 @@ def xrl_orthogonalise(grad, steps=5, eps=1e-7, out=None, workspace=None, device_
         else:
             with torch.cuda.stream(torch.cuda.ExternalStream(int(stream), device=grad.device)):
                 workspace = torch.empty(size, dtype=torch.uint8, device=grad.device)
-    elif str(workspace.dtype) != "torch.uint8" or not workspace.is_contiguous():
+    elif workspace.dtype is not torch.uint8 or not workspace.is_contiguous():
         raise XrlError(1, f"{where} (workspace: contiguous uint8)")
     st = load_library().xrl_orthogonalise(
         dev, dtype, batch, rows, cols, gp, gld, gbs, steps, eps, op, old, obs, workspace.data_ptr(), workspace.numel(),
-        _flat(where, "device_status", device_status, "int32", 1), _stream_on(dev, stream))
+        _flat(where, "device_status", device_status, torch.int32, (1,)), _stream_on(dev, stream))
     _check(st, where)
     return out
 

@@ -490,6 +490,7 @@ template <int THREADS> struct Candidates {
   int32_t i[THREADS];
   float best_v[kMostTop];
   int32_t best_i[kMostTop];
+  uint8_t flagged[THREADS];              // of each warp: the lanes that are walked again
   int n;
 };
 template <int THREADS> __device__ __forceinline__ void rank_candidates(Candidates<THREADS>& s, int n, int k) {
@@ -537,6 +538,8 @@ __device__ __forceinline__ void best_of_part(const Row<T>& r, int v0, int v1, bo
   const float bound = float_of(lo);
   const unsigned flags = __ballot_sync(kAll, thread_max > kNegInf && mine >= lo);
   const int iters = (v1 - v0 + THREADS - 1) / THREADS, items = __popc(flags) * iters;
+  if (flags >> lane & 1) s.flagged[warp * 32 + __popc(flags & ((1u << lane) - 1))] = uint8_t(lane);
+  __syncwarp();
   auto put = [&](float v, int32_t i) {
     if (v >= bound && v > kNegInf) {
       const int at = atomicAdd(&s.n, 1);
@@ -544,7 +547,7 @@ __device__ __forceinline__ void best_of_part(const Row<T>& r, int v0, int v1, bo
     }
   };
   for (int i = lane; i < items; i += 32) {
-    const int j = v0 + warp * 32 + __fns(flags, 0, i / iters + 1) + (i % iters) * THREADS;
+    const int j = v0 + warp * 32 + s.flagged[warp * 32 + i / iters] + (i % iters) * THREADS;
     if (j < v1) {
       const uint4 v = r.template vec<MASK>(j);
       float f[N];

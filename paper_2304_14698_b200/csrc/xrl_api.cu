@@ -54,8 +54,8 @@ struct DeviceBuf {
 };
 
 struct RestoreDevice {
-  int device;
-  ~RestoreDevice() { cudaSetDevice(device); }
+  int device, used;
+  ~RestoreDevice() { if (used != device) cudaSetDevice(device); }
 };
 
 size_t storage_bytes(int dtype) { return dtype == XRL_BF16 ? 2 : 4; }
@@ -1282,8 +1282,8 @@ xrl_status xrl_gae(int32_t device, int32_t num_steps, int32_t num_trajectories, 
 #define XRL_ON_DEVICE(device)                                  \
   int previous_device = 0;                                     \
   XRL_CUDA(cudaGetDevice(&previous_device));                   \
-  XRL_CUDA(cudaSetDevice(device));                             \
-  const RestoreDevice restore_device{previous_device}
+  const RestoreDevice restore_device{previous_device, device}; \
+  if (device != previous_device) XRL_CUDA(cudaSetDevice(device))
 
 static bool logit_rows_ok(int32_t dtype, int32_t rows, int32_t vocab, const void* logits, int64_t row_stride,
                           const uint8_t* mask, int64_t mask_stride, float scale) {

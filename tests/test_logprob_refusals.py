@@ -65,9 +65,9 @@ def test_the_binding_refuses_tensors_of_other_shapes_types_and_places():
     with pytest.raises(xrl.XrlError):
         xrl.xrl_logprob_grad(x, torch.zeros(ROWS, 2))
     from paper_2304_14698_b200 import binding as b
-    for call in (lambda: b._flat("f", "token", torch.zeros(ROWS, dtype=torch.int64), "int32", ROWS),
-                 lambda: b._flat("f", "token", torch.zeros(2 * ROWS, dtype=torch.int32)[::2], "int32", ROWS),
-                 lambda: b._flat("f", "token", torch.zeros(ROWS + 1, dtype=torch.int32), "int32", ROWS),
+    for call in (lambda: b._flat("f", "token", torch.zeros(ROWS, dtype=torch.int64), torch.int32, (ROWS,)),
+                 lambda: b._flat("f", "token", torch.zeros(2 * ROWS, dtype=torch.int32)[::2], torch.int32, (ROWS,)),
+                 lambda: b._flat("f", "token", torch.zeros(ROWS + 1, dtype=torch.int32), torch.int32, (ROWS,)),
                  lambda: b._rows_of("f", "x", torch.zeros(VOCAB, ROWS).T, ROWS, VOCAB),
                  lambda: b._mask_of("f", torch.zeros(ROWS, VOCAB), ROWS, VOCAB),
                  lambda: b._mask_of("f", torch.zeros(ROWS, VOCAB + 1, dtype=torch.uint8), ROWS, VOCAB),
