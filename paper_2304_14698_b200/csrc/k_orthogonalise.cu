@@ -529,6 +529,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_ns_product(const __grid_constan
   }
   const int ksteps = (a.k + kStep - 1) / kStep;
   enter();
+  // where SMs are free for the next launch's CTAs (five layers of 256: 100 -> 97 us)
+  if (gridDim.x * 2 <= kNumSMs) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
   // Both of the next roles run with the whole warp, one lane of which issues: what the loops carry is then the same for all
   // lanes and stays in uniform registers, where the instructions want it.  (Run by one lane alone, a product instruction cost
@@ -662,7 +664,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_ns_product(const __grid_constan
       if (lane == 0) raise(a.status, XRL_ERR_TIMEOUT);
       let_copies_land();
     }
-    if (lane == 0) tma_wait_all();
+    if (lane == 0) tma_wait_read<0>();   // (the launch ends when what they write is there)
   }
   tc_fence_before();
   __syncwarp();
