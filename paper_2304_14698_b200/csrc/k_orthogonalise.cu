@@ -127,6 +127,7 @@ struct NsArgs {
   int m, n, k;                           // of the product
   int tiles_n, tiles;                    // per matrix; symmetric products: tiles on and above the diagonal
   int total;                             // tiles of all matrices
+  int parts;                             // CTAs that share a tile's reduction (SPLIT)
   float descale;                         // accumulator -> value
   float gain;                            // accumulator -> its share of the scaled result
   const float* diag_in;                  // [batch][diag_stride]
@@ -146,12 +147,14 @@ constexpr int kBlockBytes = 32 * 32 * 2; // a 32 x 32 piece of an epilogue warp:
 // and N / 2 of the right one, so a tile of 256 x 256 asks half of what four of 128 x 128 do of L2.
 // CHUNK: stages whose products stay in one accumulator.  The tensor cores cut the sum after each instruction instead of
 // rounding it, which shrinks a sum of n instructions by about n / 4 units in its last place (fp32, 32 x 8,192 in one
-// accumulator: 4e-5 of the update).  fp32 updates therefore add the accumulators of 256 entries of the reduction in registers,
-// and issue the small products of a stage first, onto a small sum.
+// accumulator: 4e-5 of the update).  fp32 updates therefore add the accumulators of 128 or 256 entries of the reduction in
+// registers, and issue the small products of a stage first, onto a small sum.  (256: five layers of 256 98 us and an error of
+// 1.6e-6, 128: 100 and 8e-7, plain fp32 products 1.6e-6; for the pairs' larger matrices 256 costs 557 us, 128 643, errors 1.2e-6
+// and 6e-7 where plain products have 3.3e-6.)
 template <int CTAS, int COLS, int NPROD> struct Cfg {
   static constexpr int M = CTAS * kRows, N = COLS;
   static constexpr int SUB = M / N;                       // tiles side by side in a square of M x M
-  static constexpr int CHUNK = NPROD == 1 ? 1 << 30 : 4;
+  static constexpr int CHUNK = NPROD == 1 ? 1 << 30 : CTAS == 1 ? 2 : 4;
   static constexpr int B_ROWS = N / CTAS;
   static constexpr int A_BYTES = kRows * kStep * 2, B_BYTES = B_ROWS * kStep * 2;
   static constexpr int PARTS = NPROD == 1 ? 1 : 2;        // hi; hi and lo
@@ -481,14 +484,21 @@ __device__ __forceinline__ void prefetch_map(const CUtensorMap* m) {
   asm volatile("prefetch.tensormap [%0];" ::"l"(m) : "memory");
 }
 
-template <int CTAS, int COLS, int MODE, bool TALL, int NPROD>
+constexpr int kDumpPitch = 68 * 4;       // bytes of a row of a tile's 64 fp32 columns
+
+// SPLIT: a cluster of up to eight CTAs shares a tile of a long reduction, a stretch of it each; the accumulators then meet
+// through the cluster's shared memory, each CTA adding up (always in the same order) and finishing some of the tile's eight
+// pieces.  For Gram matrices of few tiles.
+template <int CTAS, int COLS, int MODE, bool TALL, int NPROD, bool SPLIT>
 __global__ void __launch_bounds__(kThreads, 1) k_ns_product(const __grid_constant__ Maps maps, const NsArgs a) {
   using C = Cfg<CTAS, COLS, NPROD>;
   constexpr bool SYM = MODE != APPLY, A_MN = MODE == GRAM && TALL, B_MN = A_MN || (MODE == APPLY && !TALL);
   extern __shared__ __align__(1024) uint8_t smem[];
   const uint32_t base = smem_u32(smem);
   const int warp = __shfl_sync(0xFFFFFFFFu, int(threadIdx.x) >> 5, 0), lane = threadIdx.x & 31;
-  const int rank = int(blockIdx.x) % CTAS, first = int(blockIdx.x) / CTAS, step = int(gridDim.x) / CTAS;
+  const int group = SPLIT ? a.parts : CTAS;
+  const int rank = SPLIT ? 0 : int(blockIdx.x) % CTAS, part = SPLIT ? int(blockIdx.x) % group : 0;
+  const int first = int(blockIdx.x) / group, step = int(gridDim.x) / group;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + C::OFF_TMEM);
   auto bar_full = [&](int s) { return base + C::OFF_BAR + 8u * s; };
   auto bar_empty = [&](int s) { return base + C::OFF_BAR + 8u * (C::STAGES + s); };
@@ -527,7 +537,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_ns_product(const __grid_constan
     total = 0;
     if (threadIdx.x == 0) raise(a.status, XRL_ERR_UNSUPPORTED);
   }
-  const int ksteps = (a.k + kStep - 1) / kStep;
+  const int all_ksteps = (a.k + kStep - 1) / kStep;
+  const int kbegin = SPLIT ? all_ksteps * part / group : 0;
+  const int ksteps = SPLIT ? all_ksteps * (part + 1) / group - kbegin : all_ksteps;
   enter();
   // where SMs are free for the next launch's CTAs (five layers of 256: 100 -> 97 us)
   if (gridDim.x * 2 <= kNumSMs) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -549,11 +561,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_ns_product(const __grid_constan
         const uint32_t at = base + s * C::STAGE;
         if (elected()) {
           if (rank == 0) mbar_expect_tx(bar_full(s), CTAS * C::STAGE);
-          load_operand<CTAS, A_MN, kRows>(at, &maps.a_hi, row, k * kStep, t.z, bar_full(s));
-          load_operand<CTAS, B_MN, C::B_ROWS>(at + C::OFF_B, &maps.b_hi, col, k * kStep, t.z, bar_full(s));
+          load_operand<CTAS, A_MN, kRows>(at, &maps.a_hi, row, (kbegin + k) * kStep, t.z, bar_full(s));
+          load_operand<CTAS, B_MN, C::B_ROWS>(at + C::OFF_B, &maps.b_hi, col, (kbegin + k) * kStep, t.z, bar_full(s));
           if (NPROD > 1) {
-            load_operand<CTAS, A_MN, kRows>(at + C::A_BYTES, &maps.a_lo, row, k * kStep, t.z, bar_full(s));
-            load_operand<CTAS, B_MN, C::B_ROWS>(at + C::OFF_B + C::B_BYTES, &maps.b_lo, col, k * kStep, t.z, bar_full(s));
+            load_operand<CTAS, A_MN, kRows>(at + C::A_BYTES, &maps.a_lo, row, (kbegin + k) * kStep, t.z, bar_full(s));
+            load_operand<CTAS, B_MN, C::B_ROWS>(at + C::OFF_B + C::B_BYTES, &maps.b_lo, col, (kbegin + k) * kStep, t.z, bar_full(s));
           }
         }
         __syncwarp();
@@ -642,21 +654,35 @@ __global__ void __launch_bounds__(kThreads, 1) k_ns_product(const __grid_constan
           for (int i = 0; i < (NPROD == 1 ? 1 : WC); ++i) sum[i] = (k0 == 0 ? 0.f : sum[i]) + __uint_as_float(v[i]);
           k0 = k1;
           if (k1 < ksteps) continue;
-          if constexpr (NPROD > 1) {
+          if constexpr (NPROD > 1 && !SPLIT) {
 #pragma unroll
             for (int c = 0; c < WC; c += 16) tc_st16(taddr + c, sum + c);
           }
-          asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+          if (!SPLIT) asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
         }
+        if constexpr (SPLIT) {
+          uint32_t v[32];
+          if (NPROD > 1 && ksteps > C::CHUNK) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(sum[NPROD == 1 ? 0 : i]);
+          } else {
+            tc_ld32(taddr, v);
+            tc_wait_ld();
+          }
+          uint8_t* to = smem + (q * 32 + lane) * kDumpPitch + side * 128;      // where the stages were: all are multiplied
+#pragma unroll
+          for (int i = 0; i < 32; i += 4) *reinterpret_cast<uint4*>(to + 4 * i) = make_uint4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+        } else {
 #pragma unroll 1
-        for (int c = 0; ok && c < WC; c += 32) {
-          if (c) ask<MODE>(maps, a, w, t.z, row, col + c);
+          for (int c = 0; ok && c < WC; c += 32) {
+            if (c) ask<MODE>(maps, a, w, t.z, row, col + c);
+            __syncwarp();
+            ok = finish<MODE, TALL, NPROD>(maps, a, w, t, row, col + c, taddr + c);
+          }
+          tc_fence_before();
           __syncwarp();
-          ok = finish<MODE, TALL, NPROD>(maps, a, w, t, row, col + c, taddr + c);
+          if (lane == 0) arrive_first<CTAS>(bar_acc_empty(buf));
         }
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) arrive_first<CTAS>(bar_acc_empty(buf));
         k0 = k1;
       }
     }
@@ -665,6 +691,44 @@ __global__ void __launch_bounds__(kThreads, 1) k_ns_product(const __grid_constan
       let_copies_land();
     }
     if (lane == 0) tma_wait_read<0>();   // (the launch ends when what they write is there)
+  }
+  if constexpr (SPLIT) {
+    __syncwarp();
+    tile_sync<2>();
+    const int share = 8 / group, worker = warp - 2;
+    if (worker >= 0 && worker < share && first < total) {
+      const Tile t = tile_of<C::M, C::N, SYM>(a, first);
+      const int piece = part * share + worker, q = piece & 3, side = piece >> 2;
+      const uint32_t from = base + (q * 32 + lane) * kDumpPitch + side * 128;
+      float sum[32];
+#pragma unroll
+      for (int i = 0; i < 32; ++i) sum[i] = 0.f;
+#pragma unroll 1
+      for (int p = 0; p < group; ++p) {
+        uint32_t at;
+        asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(from), "r"(p));
+#pragma unroll
+        for (int i = 0; i < 32; i += 4) {
+          float x, y, z, w;
+          asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                       : "=f"(x), "=f"(y), "=f"(z), "=f"(w) : "r"(at + 4 * i) : "memory");
+          sum[i] += x; sum[i + 1] += y; sum[i + 2] += z; sum[i + 3] += w;
+        }
+      }
+      tc_fence_after();
+      const uint32_t taddr = tmem_base + (uint32_t((warp & 3) * 32) << 16);    // as a place to turn rows into 8 x 8 blocks
+      tc_st16(taddr, sum);
+      tc_st16(taddr + 16, sum + 16);
+      asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+      Pieces w;
+      w.hi = base + C::OFF_BLOCKS + worker * 2 * kBlockBytes;
+      w.bar = bar_in(worker);
+      w.lane = lane;
+      finish<MODE, TALL, NPROD>(maps, a, w, t, t.row + q * 32, t.col + side * 32, taddr);
+      if (lane == 0) tma_wait_read<0>();
+    }
+    __syncwarp();
+    tile_sync<2>();                      // nobody leaves while its accumulators are read
   }
   tc_fence_before();
   __syncwarp();
@@ -700,18 +764,19 @@ bool make_operand(CUtensorMap* hi, CUtensorMap* lo, const Operand& o, int batch,
   return make_map3(hi, o.p.hi, batch, o.rows, o.cols, o.ld, box) && (!both || make_map3(lo, o.p.lo, batch, o.rows, o.cols, o.ld, box));
 }
 
-template <int CTAS, int COLS, int MODE, bool TALL, int NPROD>
-bool launch_tiles(const Maps& maps, NsArgs a, int batch, cudaStream_t st) {
+template <int CTAS, int COLS, int MODE, bool TALL, int NPROD, bool SPLIT = false>
+bool launch_tiles(const Maps& maps, NsArgs a, int batch, cudaStream_t st, int parts = 1) {
   using C = Cfg<CTAS, COLS, NPROD>;
   static bool done[64] = {};
-  if (!ensure_dynamic_smem(k_ns_product<CTAS, COLS, MODE, TALL, NPROD>, C::SMEM_BYTES, done)) return false;
+  if (!ensure_dynamic_smem(k_ns_product<CTAS, COLS, MODE, TALL, NPROD, SPLIT>, C::SMEM_BYTES, done)) return false;
   const int tm = (a.m + C::M - 1) / C::M;
   a.tiles_n = (a.n + C::N - 1) / C::N;
   a.tiles = MODE == APPLY ? tm * a.tiles_n : tm * (tm + 1) / 2 * C::SUB;
   a.total = a.tiles * batch;
-  const int most = kNumSMs / CTAS;
+  a.parts = parts;
+  const int cluster = CTAS * parts, most = kNumSMs / cluster;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = unsigned((a.total < most ? a.total : most) * CTAS);
+  cfg.gridDim = unsigned((a.total < most ? a.total : most) * cluster);
   cfg.blockDim = kThreads;
   cfg.dynamicSmemBytes = C::SMEM_BYTES;
   cfg.stream = st;
@@ -719,11 +784,11 @@ bool launch_tiles(const Maps& maps, NsArgs a, int batch, cudaStream_t st) {
   at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   at[0].val.programmaticStreamSerializationAllowed = 1;
   at[1].id = cudaLaunchAttributeClusterDimension;
-  at[1].val.clusterDim.x = CTAS;
+  at[1].val.clusterDim.x = cluster;
   at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
   cfg.attrs = at;
-  cfg.numAttrs = CTAS > 1 ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, k_ns_product<CTAS, COLS, MODE, TALL, NPROD>, maps, a) == cudaSuccess;
+  cfg.numAttrs = cluster > 1 ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, k_ns_product<CTAS, COLS, MODE, TALL, NPROD, SPLIT>, maps, a) == cudaSuccess;
 }
 
 bool make_pieces(CUtensorMap* hi, CUtensorMap* lo, const Operand& o, int batch) {
@@ -750,6 +815,15 @@ bool launch_product(const Operand& left, const Operand& right, const Operand* in
     return false;
   if (kind == 2) return launch_tiles<2, WIDE, MODE, TALL, NPROD>(maps, a, batch, st);
   if (NPROD == 1 && kind == 1) return launch_tiles<1, NPROD == 1 ? 128 : 64, MODE, TALL, NPROD>(maps, a, batch, st);
+  if constexpr (MODE == GRAM) {
+    // One tile to a cluster, and shares that are worth the meeting, some 3 us: 12 stages of one product or 5 of three
+    // (fp32 49 x 1,270 109 -> 100 us, bf16 4,100 x 1,001 228 -> 209; but fp32 256 x 512 in two 107 -> 111, bf16 128 x 1,024 in
+    // four 70 -> 84).
+    int parts = 1;
+    while (parts < 8 && tiles(128, 64) * parts * 2 <= kNumSMs && (a.k + kStep - 1) / kStep >= (NPROD == 1 ? 24 : 10) * parts)
+      parts *= 2;
+    if (parts > 1) return launch_tiles<1, 64, MODE, TALL, NPROD, true>(maps, a, batch, st, parts);
+  }
   return launch_tiles<1, 64, MODE, TALL, NPROD>(maps, a, batch, st);
 }
 

@@ -161,3 +161,14 @@ def test_the_same_bits_every_time_on_streams_in_graphs_and_with_workspaces():
 def test_empty_batches():
     for shape in ((0, 5, 5), (2, 0, 5), (2, 5, 0)):
         assert xrl.xrl_orthogonalise(torch.zeros(shape, device="cuda")).shape == shape
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("shape", [(1, 16, 4000), (1, 4000, 16), (3, 130, 2100), (1, 2100, 130), (1, 500, 1111), (1, 100, 513), (8, 64, 900),
+                                   (1, 60, 32768), (1, 1, 5000)])
+def test_long_reductions_are_shared_out(dtype, shape):
+    for kind in ("gradient", "normal"):
+        g = make(dtype, *shape, seed=shape[1], kind=kind)
+        got = xrl.xrl_orthogonalise(g)
+        assert off(got, define(g)) <= TOL[dtype], kind
+        assert torch.equal(xrl.xrl_orthogonalise(g), got)
