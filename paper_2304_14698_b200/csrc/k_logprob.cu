@@ -285,9 +285,7 @@ __device__ __forceinline__ void mask_words(const uint8_t* p, uint32_t& m0, uint3
   if (N == 8) m1 = __funnelshift_r(w1, off ? __ldg(w + 2) : 0u, off);
 }
 // ---- a thread's own copies ahead: what it will read, on its way to its own places in shared memory ------------------
-// Registers for two chunks and four warps a scheduler do not go together, and without loads in flight during the
-// arithmetic the rows come at half of HBM's rate (8,192 x 32,000 bf16 156 us).  cp.async needs neither registers nor, as no
-// thread reads another's places, barriers.
+// cp.async needs neither registers nor, as no thread reads another's places, barriers.
 template <int BYTES> __device__ __forceinline__ void copy_ahead(uint32_t dst, const void* src) {
   if (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
   else asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
@@ -295,8 +293,8 @@ template <int BYTES> __device__ __forceinline__ void copy_ahead(uint32_t dst, co
 __device__ __forceinline__ void copies_end_group() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 // DEPTH groups of U vectors per thread, each with the words of its mask
-template <typename T, int THREADS, int U, bool MASK> struct Ahead {
-  static constexpr int DEPTH = 3, N = Vec<T>::N, WORDS = MASK ? N / 4 + 1 : 0;
+template <typename T, int THREADS, int U> struct Ahead {
+  static constexpr int DEPTH = 3, N = Vec<T>::N, WORDS = N / 4 + 1;
   static constexpr int VEC_BYTES = THREADS * 16, WORD_BYTES = THREADS * 4;
   static constexpr int GROUP_BYTES = U * (VEC_BYTES + WORDS * WORD_BYTES);
   static constexpr int BYTES = DEPTH * GROUP_BYTES;
@@ -309,26 +307,22 @@ template <typename T, int THREADS, int U, bool MASK> struct Ahead {
   }
   __device__ __forceinline__ void ask(int group, int u, const T* x, const uint8_t* mask) const {
     copy_ahead<16>(vec_at(group, u), x);
-    if (MASK) {
-      const uintptr_t at = reinterpret_cast<uintptr_t>(mask);
-      const uint32_t* w = reinterpret_cast<const uint32_t*>(at & ~uintptr_t(3));
+    const uintptr_t at = reinterpret_cast<uintptr_t>(mask);
+    const uint32_t* w = reinterpret_cast<const uint32_t*>(at & ~uintptr_t(3));
 #pragma unroll
-      for (int i = 0; i < WORDS; ++i)
-        if (i + 1 < WORDS || (at & 3)) copy_ahead<4>(word_at(group, u, i), w + i);
-    }
+    for (int i = 0; i < WORDS; ++i)
+      if (i + 1 < WORDS || (at & 3)) copy_ahead<4>(word_at(group, u, i), w + i);
   }
   __device__ __forceinline__ uint4 take(int group, int u, const uint8_t* mask) const {
     uint4 v;
     asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(vec_at(group, u)) : "memory");
-    if (MASK) {
-      const uint32_t off = uint32_t(reinterpret_cast<uintptr_t>(mask) & 3) * 8;
-      uint32_t w[3] = {0u, 0u, 0u};
+    const uint32_t off = uint32_t(reinterpret_cast<uintptr_t>(mask) & 3) * 8;
+    uint32_t w[3] = {0u, 0u, 0u};
 #pragma unroll
-      for (int i = 0; i < WORDS; ++i)
-        asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w[i]) : "r"(word_at(group, u, i)) : "memory");
-      // (the last word is another call's where nothing was asked for; no bit of it is used then)
-      Vec<T>::drop(v, __funnelshift_r(w[0], w[1], off), N == 8 ? __funnelshift_r(w[1], w[2], off) : 0u);
-    }
+    for (int i = 0; i < WORDS; ++i)
+      asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w[i]) : "r"(word_at(group, u, i)) : "memory");
+    // (the last word is whatever lay there where nothing was asked for; no bit of it is used then)
+    Vec<T>::drop(v, __funnelshift_r(w[0], w[1], off), N == 8 ? __funnelshift_r(w[1], w[2], off) : 0u);
     return v;
   }
 };
@@ -591,98 +585,52 @@ __device__ __forceinline__ void best_of_part(const Row<T>& r, int v0, int v1, bo
   rank_candidates<THREADS>(s, n, k);
 }
 
-// A CTA takes rows first, first + step, ... (parts > 1: a cluster takes one row, each CTA a part of it).
-template <typename T, int THREADS, int U, bool MASK, bool TOP>
-__global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_logprob_cta(RowArgs a, RowOut o, int log_parts) {
-  using A = Ahead<T, THREADS, U, MASK>;
+// A CTA takes a row (parts > 1: a cluster does, each CTA a part of it).  What hides the loads is other CTAs' arithmetic:
+// copies into shared memory ahead of it, by CTAs that stay for many rows, came to 115 us where this takes 92 (8,192 x 32,000 bf16).
+template <typename T, int THREADS, int U, int CTAS, bool MASK, bool TOP>
+__global__ void __launch_bounds__(THREADS, CTAS) k_logprob_cta(RowArgs a, RowOut o, int log_parts) {
   enter();
-  constexpr int N = Vec<T>::N, W = THREADS / 32;
-  extern __shared__ __align__(16) uint8_t s_ahead[];
-  __shared__ Sums s_sums[2][W];          // of this row and of the one before, which a warp may still read
+  constexpr int N = Vec<T>::N, W = THREADS / 32, GROUP = U * THREADS;
+  __shared__ Sums s_sums[W];
   __shared__ float s_red[64];
   __shared__ Candidates<TOP ? THREADS : 32> s_best;
   __shared__ Sums s_part;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int parts = 1 << log_parts, part = parts > 1 ? int(cluster_rank()) : 0;
-  const int64_t step = parts > 1 ? a.rows : int64_t(gridDim.x);
   // part p of a row's vectors starts here (below 2^29 vectors and 8 parts: 32 bits)
   auto start_of = [&](int vecs, int p) { return int((uint32_t(vecs) * uint32_t(p)) >> log_parts); };
   const float c = a.scale * kLog2e;
   // (as a bf16 number, which it is for both types; rounded, it is within 2^-9 of itself)
   const float floor = to_float(bf16(kLowest / c));
   const Sums zero = {kNegInf, floor * c, 0.f, 0.f};
-  const A ahead(s_ahead);
 
-  // what is asked for next: of row p_row, from p_x and p_mask on (the thread's own vector), the p_left vectors that are left
-  constexpr int GROUP = U * THREADS;
-  int64_t p_row = blockIdx.x >> log_parts;
-  int p_group = 0, p_left = 0;
-  const T* p_x = nullptr;
-  const uint8_t* p_mask = nullptr;
-  auto p_start = [&]() {
-    p_left = 0;
-    if (p_row >= a.rows) return;
-    const Row<T> r(a, p_row, MASK);
-    const int v0 = start_of(r.vecs, part);
-    p_left = start_of(r.vecs, part + 1) - v0;
-    const int64_t at = r.head + (int64_t(v0) + threadIdx.x) * N;
-    p_x = r.x + at;
-    if (MASK) p_mask = r.mask + at;
-  };
-  auto ask = [&]() {                     // one group (an empty one where a row has no whole vectors, or behind the last row)
-    if (p_left >= GROUP) {
-#pragma unroll
-      for (int u = 0; u < U; ++u) ahead.ask(p_group, u, p_x + u * THREADS * N, p_mask + u * THREADS * N);
-    } else {
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (u * THREADS + int(threadIdx.x) < p_left) ahead.ask(p_group, u, p_x + u * THREADS * N, p_mask + u * THREADS * N);
-    }
-    copies_end_group();
-    p_group = p_group + 1 < A::DEPTH ? p_group + 1 : 0;
-    p_x += GROUP * N;
-    if (MASK) p_mask += GROUP * N;
-    p_left -= GROUP;
-    if (p_left <= 0) {
-      p_row += step;
-      p_start();
-    }
-  };
-  int64_t row = p_row;
-  p_start();
-#pragma unroll
-  for (int d = 0; d < A::DEPTH - 1; ++d) ask();
-
-  int group = 0, turn = 0;
-  for (; row < a.rows; row += step, turn ^= 1) {
+  const int64_t row = blockIdx.x >> log_parts;
   const Row<T> r(a, row, MASK);
   Given given;
   if (threadIdx.x == 0 && part == 0) given = given_of<T>(a, row);
   const int v0 = start_of(r.vecs, part), v1 = start_of(r.vecs, part + 1);
-  const uint8_t* mask = MASK ? r.mask + r.head + (int64_t(v0) + threadIdx.x) * N : nullptr;
   Sums q = zero;
-  int left = v1 - v0;
-  do {
-    ask();                               // into the group taken last
-    copies_wait<A::DEPTH - 1>();
+  int j = v0 + threadIdx.x;              // the thread's next vector
+  for (int left = v1 - v0; left > 0; left -= GROUP, j += GROUP) {
     if (left >= GROUP) {
       uint4 v[U];
 #pragma unroll
-      for (int u = 0; u < U; ++u) v[u] = ahead.take(group, u, mask + u * THREADS * N);
+      for (int u = 0; u < U; ++u) v[u] = r.template vec<MASK>(j + u * THREADS);
       add_chunk<T, U>(q, v, c, floor);
-    } else if (warp * 32 < left) {       // the warp has vectors here
+    } else if (2 * left > GROUP) {
+      uint4 v[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) v[u] = j + u * THREADS < v1 ? r.template vec<MASK>(j + u * THREADS) : Vec<T>::none();
+      add_chunk<T, U>(q, v, c, floor);
+    } else {
 #pragma unroll 1
       for (int u = 0; u < U; ++u) {
-        const int at = u * THREADS + int(threadIdx.x);
-        if (at - lane >= left) break;
-        const uint4 v[1] = {at < left ? ahead.take(group, u, mask + u * THREADS * N) : Vec<T>::none()};
+        if (j + u * THREADS - lane >= v1) break;         // no vector for the whole warp
+        const uint4 v[1] = {j + u * THREADS < v1 ? r.template vec<MASK>(j + u * THREADS) : Vec<T>::none()};
         add_chunk<T, 1>(q, v, c, floor);
       }
     }
-    group = group + 1 < A::DEPTH ? group + 1 : 0;
-    if (MASK) mask += GROUP * N;
-    left -= GROUP;
-  } while (left > 0);
+  }
   const float thread_max = q.m;          // (of its whole vectors)
   if (part == 0 && threadIdx.x < 16) {
     const int j = r.edge(threadIdx.x);
@@ -692,9 +640,9 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_logprob_cta(RowArgs
     }
   }
   q = join_warp(q);
-  if (lane == 0) s_sums[turn][warp] = q;
+  if (lane == 0) s_sums[warp] = q;
   __syncthreads();
-  q = lane < W ? s_sums[turn][lane] : zero;
+  q = lane < W ? s_sums[lane] : zero;
   float largest = max_warp(q.m);
   if (TOP) best_of_part<T, TOP ? THREADS : 32, MASK>(r, v0, v1, part == 0, thread_max, largest, o.top, s_best, reinterpret_cast<uint32_t*>(s_red));
   if (parts > 1 || warp == 0) q = join_warp(q);
@@ -723,7 +671,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_logprob_cta(RowArgs
       }
     }
     cluster_arrive_wait();               // nobody leaves, and nothing is written again, while it is read
-    if (part != 0) break;
+    if (part != 0) return;
     if (TOP) rank_candidates(s_best, parts * kMostTop, o.top);
   }
   if (largest > kNegInf && largest < INFINITY && !(largest * c > kLow && largest * c < kHigh)) {       // (all threads agree)
@@ -733,7 +681,6 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_logprob_cta(RowArgs
       if (lane == 0) write_row(a, o, row, given, n, entropy_of(q));
       if (TOP) write_top(a, o, row, n, Best{s_best.best_v[lane], s_best.best_i[lane]}, lane);
     }
-    __syncthreads();
   } else if (warp == 0) {
     RowNorm n = {kNegInf, kNegInf};
     float entropy = 0.f;
@@ -745,9 +692,6 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_logprob_cta(RowArgs
     if (lane == 0) write_row(a, o, row, given, n, entropy);
     if (TOP) write_top(a, o, row, n, Best{s_best.best_v[lane], s_best.best_i[lane]}, lane);
   }
-  if (TOP) __syncthreads();              // the next row's use of the candidates
-  }
-  copies_wait<0>();
 }
 
 // ---- gradient ---------------------------------------------------------------------------------------------------
@@ -889,11 +833,32 @@ __global__ void __launch_bounds__(256) k_logprob_grad(RowArgs a, GradArgs g, int
   }
 }
 
-// Long rows: resident CTAs take pieces of rows in turn, each `piece` vectors, copied ahead across pieces; what a row shares
-// is asked for a piece ahead too.
-template <typename T, int THREADS, int U, bool MASK>
+// Long rows: a CTA takes THREADS x U vectors of one.
+template <typename T, int THREADS, int U, int CTAS>
+__global__ void __launch_bounds__(THREADS, CTAS) k_logprob_grad_cta(RowArgs a, GradArgs g, int pieces) {
+  enter();
+  constexpr int N = Vec<T>::N;
+  const int64_t row = int64_t(blockIdx.x / uint32_t(pieces));
+  const int v0 = int(blockIdx.x - uint32_t(row) * uint32_t(pieces)) * U * THREADS, j0 = v0 + int(threadIdx.x);
+  const Row<T> r(a, row, false);
+  const RowInputs in = inputs_of(a, g, row);
+  uint4 v[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) v[u] = j0 + u * THREADS < r.vecs ? r.template vec<false>(j0 + u * THREADS) : Vec<T>::none();
+  T* out = static_cast<T*>(g.grad) + row * g.grad_stride;
+  const RowGrad f(a, in);
+  const bool whole = aligned16(out + r.head);
+#pragma unroll
+  for (int u = 0; u < U; ++u)
+    if (j0 + u * THREADS < r.vecs) grad_vector(f, v[u], r.head + (j0 + u * THREADS) * N, out, whole);
+  if (v0 == 0) grad_edges(f, r, out, threadIdx.x);
+}
+
+// Long masked rows: resident CTAs take pieces of rows in turn, each `piece` vectors, copied ahead across pieces with their
+// mask bytes; what a row shares is asked for a piece ahead too.
+template <typename T, int THREADS, int U>
 __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_logprob_grad_rows(RowArgs a, GradArgs g, int pieces, int piece) {
-  using A = Ahead<T, THREADS, U, MASK>;
+  using A = Ahead<T, THREADS, U>;
   enter();
   constexpr int N = Vec<T>::N, GROUP = U * THREADS;
   extern __shared__ __align__(16) uint8_t s_ahead[];
@@ -913,11 +878,11 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_logprob_grad_rows(R
     int64_t row;
     int v0;
     split(p_unit, row, v0);
-    const Row<T> r(a, row, MASK);
+    const Row<T> r(a, row, true);
     p_left = min(r.vecs - v0, piece);
     const int64_t at = r.head + (int64_t(v0) + threadIdx.x) * N;
     p_x = r.x + at;
-    if (MASK) p_mask = r.mask + at;
+    p_mask = r.mask + at;
   };
   auto ask = [&]() {
     if (p_left >= GROUP) {
@@ -931,7 +896,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_logprob_grad_rows(R
     copies_end_group();
     p_group = p_group + 1 < A::DEPTH ? p_group + 1 : 0;
     p_x += GROUP * N;
-    if (MASK) p_mask += GROUP * N;
+    p_mask += GROUP * N;
     p_left -= GROUP;
     if (p_left <= 0) {
       p_unit += gridDim.x;
@@ -952,7 +917,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_logprob_grad_rows(R
   for (int64_t unit = blockIdx.x; unit < units; unit += gridDim.x) {
     const RowGrad f(a, next);
     split(unit, row, v0);
-    const Row<T> r(a, row, MASK);
+    const Row<T> r(a, row, true);
     T* out = static_cast<T*>(g.grad) + row * g.grad_stride;
     const bool whole = aligned16(out + r.head);
     if (unit + gridDim.x < units) {
@@ -963,7 +928,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_logprob_grad_rows(R
     }
     if (v0 == 0) grad_edges(f, r, out, threadIdx.x);
     int left = min(r.vecs - v0, piece), j = r.head + (v0 + int(threadIdx.x)) * N;
-    const uint8_t* mask = MASK ? r.mask + j : nullptr;
+    const uint8_t* mask = r.mask + j;
     do {
       ask();
       copies_wait<A::DEPTH - 1>();
@@ -973,7 +938,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_logprob_grad_rows(R
           grad_vector(f, ahead.take(group, u, mask + u * THREADS * N), j + u * THREADS * N, out, whole);
       group = group + 1 < A::DEPTH ? group + 1 : 0;
       j += GROUP * N;
-      if (MASK) mask += GROUP * N;
+      mask += GROUP * N;
       left -= GROUP;
     } while (left > 0);
   }
@@ -998,33 +963,34 @@ void launch_cluster(K kernel, unsigned grid, unsigned threads, size_t smem, unsi
   cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
-template <typename T, int THREADS, int U, bool MASK, bool TOP>
-bool launch_cta(const RowArgs& a, const RowOut& o, int parts, cudaStream_t st) {
-  constexpr int SMEM = Ahead<T, THREADS, U, MASK>::BYTES;
-  static bool done[64] = {};
-  if (!ensure_dynamic_smem(k_logprob_cta<T, THREADS, U, MASK, TOP>, SMEM, done)) return false;
-  // resident CTAs: 64 registers a thread, 227 KB of shared memory
-  constexpr int FIT = (227 * 1024) / (SMEM + 8 * 1024), MOST = 1024 / THREADS < FIT ? 1024 / THREADS : FIT;
-  const int64_t work = a.rows * parts, most = parts > 1 ? work : int64_t(kNumSMs) * MOST;
-  launch_cluster(k_logprob_cta<T, THREADS, U, MASK, TOP>, unsigned(work < most ? work : most), THREADS, SMEM, parts, st, a, o,
-                 parts == 8 ? 3 : parts == 4 ? 2 : parts == 2 ? 1 : 0);
-  return true;
+template <typename T, int THREADS, int U, int CTAS, bool MASK, bool TOP>
+void launch_cta(const RowArgs& a, const RowOut& o, int log_parts, cudaStream_t st) {
+  launch_cluster(k_logprob_cta<T, THREADS, U, CTAS, MASK, TOP>, unsigned(a.rows << log_parts), THREADS, 0, 1 << log_parts, st, a, o,
+                 log_parts);
 }
+// Threads, vectors a thread has in flight, CTAs an SM holds.  Measured in us, 16,384 rows of 1,200 and 8,000, 8,192 of 32,000, bf16:
+// 64 threads by four vectors 24, 65 and -, by eight -, 49 and 88, 128 by eight 31, 60 and 84; with masks 128 by four 41, 89 and
+// 136, by eight -, 132 and 148; with alternatives, whose search is a CTA's, 128 by four 63, 83 and 111, 256 by two 112, 123 and 124,
+// but 1,000 rows of 100,000 fp32 97 and 108, 256 by four 86.
 template <typename T, bool MASK, bool TOP>
-bool launch_long(const RowArgs& a, const RowOut& o, cudaStream_t st) {
-  // Few rows: a cluster of up to 8 CTAs for each, none with less than 4,096 entries; then larger CTAs; then small ones, whose
-  // rows end one by one (8,192 x 32,000 bf16: 128 threads 114 us, 256 121; with alternatives, whose search is work for a
-  // CTA, 1,500 x 50,001 fp32 masked: 128 threads 102 us, 256 89).
-  constexpr int U = MASK ? 2 : 4, FEW = TOP ? 256 : 128;
-  int parts = 1;
-  while (parts < 8 && a.rows * parts * 2 <= 2 * kNumSMs && a.vocab / (parts * 2) >= 4096) parts *= 2;
-  if (a.rows * parts <= 2 * kNumSMs) return launch_cta<T, 512, 2, MASK, TOP>(a, o, parts, st);
-  if (a.rows <= 4 * kNumSMs) return launch_cta<T, 256, U, MASK, TOP>(a, o, 1, st);
-  return launch_cta<T, FEW, U, MASK, TOP>(a, o, 1, st);
+void launch_long(const RowArgs& a, const RowOut& o, cudaStream_t st) {
+  const int vecs = a.vocab / Vec<T>::N;
+  int log_parts = 0;                     // few rows: clusters, no CTA with less than 4,096 entries
+  while (log_parts < 3 && a.rows << (log_parts + 1) <= 2 * kNumSMs && a.vocab >> (log_parts + 1) >= 4096) ++log_parts;
+  if (log_parts == 3) launch_cta<T, 256, 4, 4, MASK, TOP>(a, o, 3, st);
+  else if (a.rows << log_parts <= 2 * kNumSMs) launch_cta<T, 512, 4, 2, MASK, TOP>(a, o, log_parts, st);
+  else if (TOP && vecs >= 6000) launch_cta<T, 256, 4, 4, MASK, TOP>(a, o, 0, st);
+  else if (TOP || (MASK && vecs >= 512 && vecs < 6000)) launch_cta<T, 128, 4, 10, MASK, TOP>(a, o, 0, st);
+  else if (vecs >= 3000) launch_cta<T, 128, 8, 7, MASK, false>(a, o, 0, st);
+  else if (vecs >= 512) launch_cta<T, 64, 8, 14, MASK, false>(a, o, 0, st);
+  else launch_cta<T, 64, 4, 20, MASK, false>(a, o, 0, st);
 }
 template <typename T, bool MASK>
 bool launch_rows(const RowArgs& a, const RowOut& o, cudaStream_t st) {
-  if (a.vocab > 1024) return o.top ? launch_long<T, MASK, true>(a, o, st) : launch_long<T, MASK, false>(a, o, st);
+  if (a.vocab > 1024) {
+    o.top ? launch_long<T, MASK, true>(a, o, st) : launch_long<T, MASK, false>(a, o, st);
+    return true;
+  }
   const int64_t ctas = (a.rows + 3) / 4;
   const unsigned grid = unsigned(ctas < (int64_t(1) << 30) ? ctas : int64_t(1) << 30);
   if (a.vocab <= 128) launch(k_logprob_warp<T, 4, MASK>, grid, 128, 0, st, a, o);
@@ -1033,17 +999,27 @@ bool launch_rows(const RowArgs& a, const RowOut& o, cudaStream_t st) {
   else launch(k_logprob_warp<T, 32, MASK>, grid, 128, 0, st, a, o);
   return true;
 }
+// In us, 8,192 x 32,000 bf16: a CTA per piece 157 without a mask, 256 with one; resident CTAs with copies ahead 200 and 232.
 template <typename T, bool MASK>
 bool launch_grad(const RowArgs& a, const GradArgs& g, cudaStream_t st) {
-  constexpr int THREADS = 256, U = MASK ? 2 : 4, SMEM = Ahead<T, THREADS, U, MASK>::BYTES;
   const int vecs = a.vocab / Vec<T>::N;
-  if (vecs >= 2 * THREADS) {             // (shorter rows leave half a group empty)
-    static bool done[64] = {};
-    if (!ensure_dynamic_smem(k_logprob_grad_rows<T, THREADS, U, MASK>, SMEM, done)) return false;
-    const int piece = 2 * U * THREADS, pieces = (vecs + piece - 1) / piece;
-    const int64_t units = a.rows * pieces, most = int64_t(kNumSMs) * (1024 / THREADS);
-    launch(k_logprob_grad_rows<T, THREADS, U, MASK>, unsigned(units < most ? units : most), THREADS, SMEM, st, a, g, pieces, piece);
-    return true;
+  if (vecs >= 512) {                     // (shorter rows leave much of a CTA idle)
+    if constexpr (MASK) {
+      constexpr int THREADS = 256, U = 2, SMEM = Ahead<T, THREADS, U>::BYTES;
+      static bool done[64] = {};
+      if (!ensure_dynamic_smem(k_logprob_grad_rows<T, THREADS, U>, SMEM, done)) return false;
+      const int piece = 2 * U * THREADS, pieces = (vecs + piece - 1) / piece;
+      const int64_t units = a.rows * pieces, most = int64_t(kNumSMs) * (1024 / THREADS);
+      launch(k_logprob_grad_rows<T, THREADS, U>, unsigned(units < most ? units : most), THREADS, SMEM, st, a, g, pieces, piece);
+      return true;
+    } else {
+      constexpr int THREADS = 128, U = 4;
+      const int pieces = (vecs + THREADS * U - 1) / (THREADS * U);
+      if (a.rows * pieces <= INT32_MAX) {
+        launch(k_logprob_grad_cta<T, THREADS, U, 10>, unsigned(a.rows * pieces), THREADS, 0, st, a, g, pieces);
+        return true;
+      }
+    }
   }
   const int segs = vecs / (32 * 4) + 1;
   const int64_t ctas = (a.rows * segs + 7) / 8;
