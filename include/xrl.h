@@ -4,7 +4,8 @@
  * of its candidate rewritten graphs, encodes them with a graph neural network, reads out one
  * vector per graph and evaluates an actor-critic policy head (masked categorical distribution
  * over the candidates plus No-Op) and a value head (paper Sections 3.3.2, 3.3.3 and 3.4).
- * This library is that path and nothing else:
+ * This library is that path, and next to it (5) what the training step of any other policy needs whose logits come from the
+ * caller's own model:
  *
  *     xrl_pack / xrl_pack_flat   Section 3.3.2  batch the graphs into one meta-graph (CSR)
  *     xrl_encode                 Section 3.4    Eq. 6 -> L x Eq. 7 -> Eq. 8
@@ -12,6 +13,8 @@
  *                                Section 3.3.3  invalid-action masking, No-Op, sampling
  *     xrl_ppo_grad, xrl_gae      Section 3.3.4  the training step's objective (Eq. 3-5) and its gradient with
  *                                               respect to every weight; advantage estimates
+ *     xrl_logprob, xrl_logprob_grad             rows of logits: log probabilities, entropy, best alternatives; gradient
+ *     xrl_orthogonalise                         updates of weight matrices, orthogonalised
  *
  * Conventions
  *  - Plain C ABI.  Every function returns an xrl_status; nothing throws, aborts or traps.
@@ -323,7 +326,7 @@ xrl_status xrl_gae(int32_t device, int32_t num_steps, int32_t num_trajectories, 
  *   token       DEVICE int32 [rows], or NULL with logp NULL: the choice whose log probability is wanted; -1 = none in this row
  *   mask        DEVICE u8 [rows x vocab] or NULL: 0 = entry is invalid and its logit, whatever it is, not looked at; rows
  *               mask_stride bytes apart, 0 = one mask for all rows
- *   scale       in (0, 1e6]
+ *   scale       from 1e-6 to 1e6
  *   logp        DEVICE fp32 [rows] or NULL: ln p of the token; 0 for token -1, -infinity outside the support, NaN for a
  *               token below -1 or at vocab and above
  *   entropy     DEVICE fp32 [rows] or NULL: H; 0 for a row without support
@@ -333,8 +336,8 @@ xrl_status xrl_gae(int32_t device, int32_t num_steps, int32_t num_trajectories, 
  *               vocab) largest logits of the support in falling order, equal ones by rising index, and their ln p; -1 and
  *               -infinity where the support has fewer
  * A row with a NaN or +infinity in its support gives NaN in logp, entropy, l and top_logp; its alternatives are the best of
- * its other entries.  The order of a row's sum depends on the sizes and on where the row lies on its 16-byte boundary alone.  Needs no context; one launch; captures
- * into a CUDA graph; nothing is allocated.  Errors: INVALID_ARG, UNSUPPORTED (num_top), CUDA. */
+ * its other entries.  The order of a row's sum depends on the sizes and on how far the row's first entry is from a 16-byte
+ * boundary alone.  Needs no context; one launch; captures into a CUDA graph; nothing is allocated.  Errors: INVALID_ARG, UNSUPPORTED (num_top), CUDA. */
 #define XRL_MAX_TOP 32
 xrl_status xrl_logprob(int32_t device, int32_t dtype, int32_t rows, int32_t vocab, const void* logits, int64_t row_stride,
                        const int32_t* token, const uint8_t* mask, int64_t mask_stride, float scale, int32_t num_top,

@@ -371,6 +371,13 @@ def _stream_on(device, stream):
     return _th()._C._cuda_getCurrentRawStream(device) if stream is None else int(stream)
 
 
+def _stream_scope(stream, device):
+    """The given stream as the current one: what is allocated inside belongs to it."""
+    th = _th()
+    s = th.cuda.ExternalStream(int(stream), device=device) if int(stream) else th.cuda.default_stream(device)
+    return th.cuda.stream(s)
+
+
 def _flat(where, what, t, dtype, shape):
     """The pointer of an argument that has to be a contiguous tensor of this type and shape (or None)."""
     if t is None:
@@ -406,6 +413,9 @@ def xrl_logprob(logits, token=None, mask=None, scale=1.0, top=0, out=None, strea
     place (an earlier call's, say)."""
     where = "xrl_logprob"
     th = _th()
+    if stream is not None and out is None and logits.is_cuda:
+        with _stream_scope(stream, logits.device):
+            return xrl_logprob(logits, token, mask, scale, top)
     if logits.dim() != 2:
         raise XrlError(1, f"{where} (logits: [rows x vocab])")
     rows, vocab = logits.shape
@@ -447,6 +457,9 @@ def xrl_logprob_grad(logits, norm, token=None, dlogp=None, entropy=None, dentrop
     and of their type, may be the logits themselves; allocated (contiguous) if None."""
     where = "xrl_logprob_grad"
     th = _th()
+    if stream is not None and grad is None and logits.is_cuda:
+        with _stream_scope(stream, logits.device):
+            return xrl_logprob_grad(logits, norm, token, dlogp, entropy, dentropy, mask, scale)
     if logits.dim() != 2:
         raise XrlError(1, f"{where} (logits: [rows x vocab])")
     rows, vocab = logits.shape
@@ -489,6 +502,9 @@ def xrl_orthogonalise(grad, steps=5, eps=1e-7, out=None, workspace=None, device_
     stream, so it is safe to let go); device_status: int32 [1] or None."""
     where = "xrl_orthogonalise"
     torch = _th()
+    if stream is not None and (out is None or workspace is None) and grad.is_cuda:
+        with _stream_scope(stream, grad.device):
+            return xrl_orthogonalise(grad, steps, eps, out, workspace, device_status)
     if grad.dim() not in (2, 3):
         raise XrlError(1, f"{where} (grad: [rows x cols] or [batch x rows x cols])")
     rows, cols = grad.shape[-2:]
@@ -502,12 +518,7 @@ def xrl_orthogonalise(grad, steps=5, eps=1e-7, out=None, workspace=None, device_
     gp, gld, gbs = _matrices_of(where, "grad", grad, batch, rows, cols)
     op, old, obs = _matrices_of(where, "out", out, batch, rows, cols)
     if workspace is None:
-        size = xrl_orthogonalise_workspace(dtype, batch, rows, cols)
-        if stream is None:
-            workspace = torch.empty(size, dtype=torch.uint8, device=grad.device)
-        else:
-            with torch.cuda.stream(torch.cuda.ExternalStream(int(stream), device=grad.device)):
-                workspace = torch.empty(size, dtype=torch.uint8, device=grad.device)
+        workspace = torch.empty(xrl_orthogonalise_workspace(dtype, batch, rows, cols), dtype=torch.uint8, device=grad.device)
     elif workspace.dtype is not torch.uint8 or not workspace.is_contiguous():
         raise XrlError(1, f"{where} (workspace: contiguous uint8)")
     st = load_library().xrl_orthogonalise(

@@ -1287,7 +1287,7 @@ xrl_status xrl_gae(int32_t device, int32_t num_steps, int32_t num_trajectories, 
 
 static bool logit_rows_ok(int32_t dtype, int32_t rows, int32_t vocab, const void* logits, int64_t row_stride,
                           const uint8_t* mask, int64_t mask_stride, float scale) {
-  return (dtype == XRL_FP32 || dtype == XRL_BF16) && rows >= 0 && vocab >= 1 && scale > 0.f && scale <= 1e6f &&
+  return (dtype == XRL_FP32 || dtype == XRL_BF16) && rows >= 0 && vocab >= 1 && scale >= 1e-6f && scale <= 1e6f &&
          (rows == 0 || logits) && reinterpret_cast<uintptr_t>(logits) % storage_bytes(dtype) == 0 &&
          (rows <= 1 || row_stride >= vocab) && (!mask || rows <= 1 || mask_stride == 0 || mask_stride >= vocab);
 }

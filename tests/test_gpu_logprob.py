@@ -349,6 +349,11 @@ def test_streams_graphs_and_no_rows():
         gr = xrl.xrl_logprob_grad(x, o["norm"], token, d, o["entropy"], d, mask=mask)
     side.synchronize()
     assert all(torch.equal(o[k], want[k]) for k in o) and torch.equal(gr, wgrad)
+    o = xrl.xrl_logprob(x, token, mask=mask, top=7, stream=side.cuda_stream)
+    gr = xrl.xrl_logprob_grad(x, o["norm"], token, d, o["entropy"], d, mask=mask, stream=side.cuda_stream)
+    side.synchronize()
+    assert all(torch.equal(o[k], want[k]) for k in o) and torch.equal(gr, wgrad)
+    assert torch.equal(xrl.xrl_logprob(x, token, mask=mask, stream=0)["logp"], want["logp"])
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
         o2 = xrl.xrl_logprob(x, token, mask=mask, top=7)

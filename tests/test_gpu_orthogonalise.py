@@ -69,6 +69,13 @@ def test_every_number_of_steps(dtype, steps):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
+def test_many_steps_stay_where_the_quintic_keeps_them(dtype):
+    """From above 0.5 the quintic stays between 0.67 and 1.21; nothing leaves that however often it is applied."""
+    s = torch.linalg.svdvals(xrl.xrl_orthogonalise(make(dtype, 200, 333, seed=9, kind="normal"), steps=64).double())
+    assert 0.65 < float(s.min()) and float(s.max()) < 1.23
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("shape", [(5, 256, 256), (7, 65, 70), (3, 700, 90), (2, 1, 1), (40, 32, 48)])
 def test_batches_are_their_matrices(dtype, shape):
     g = make(dtype, *shape, seed=1)

@@ -27,7 +27,7 @@ def grad(lib, device=0, dtype=0, rows=ROWS, vocab=VOCAB, logits=P, stride=VOCAB,
 
 
 COMMON = [dict(dtype=2), dict(dtype=-1), dict(rows=-1), dict(vocab=0), dict(logits=None), dict(stride=VOCAB - 1), dict(stride=-VOCAB),
-          dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf")), dict(scale=2e6),
+          dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf")), dict(scale=2e6), dict(scale=9e-7),
           dict(mask=P, mstride=VOCAB - 1), dict(mask=P, mstride=-1), dict(logits=P + 2), dict(logits=P + 1, dtype=1), dict(norm=P + 4)]
 
 
