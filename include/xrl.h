@@ -374,8 +374,8 @@ xrl_status xrl_logprob_grad(int32_t device, int32_t dtype, int32_t rows, int32_t
  *              per entry of G and of the smaller Gram matrix).  It holds nothing between calls; calls that may run at the
  *              same time need one each
  *   device_status  DEVICE int32 [1] or NULL: XRL_OK, or XRL_ERR_TIMEOUT if a bounded wait ran out (the results are undefined then)
- * A matrix with a NaN or an infinity becomes NaN; the others of its batch are not affected.  The results do not depend
- * on anything but the inputs, bit for bit.  Needs no context; 2 + 3 * steps launches at most; captures into a CUDA graph.
+ * A matrix with a NaN or an infinity becomes NaN; the others of its batch are not affected.  A call's results are the same
+ * bits every time; a matrix's last bits may depend on how many share its call (the tiles are chosen by that).  Needs no context; 2 + 3 * steps launches at most; captures into a CUDA graph.
  * Errors: INVALID_ARG, UNSUPPORTED (sizes), CUDA. */
 #define XRL_MAX_SIDE 32768
 xrl_status xrl_orthogonalise_workspace(int32_t dtype, int32_t batch, int32_t rows, int32_t cols, size_t* bytes);

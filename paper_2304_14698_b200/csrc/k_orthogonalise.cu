@@ -147,14 +147,19 @@ constexpr int kBlockBytes = 32 * 32 * 2; // a 32 x 32 piece of an epilogue warp:
 // and N / 2 of the right one, so a tile of 256 x 256 asks half of what four of 128 x 128 do of L2.
 // CHUNK: stages whose products stay in one accumulator.  The tensor cores cut the sum after each instruction instead of
 // rounding it, which shrinks a sum of n instructions by about n / 4 units in its last place (fp32, 32 x 8,192 in one
-// accumulator: 4e-5 of the update).  fp32 updates therefore add the accumulators of 128 or 256 entries of the reduction in
-// registers, and issue the small products of a stage first, onto a small sum.  (256: five layers of 256 98 us and an error of
-// 1.6e-6, 128: 100 and 8e-7, plain fp32 products 1.6e-6; for the pairs' larger matrices 256 costs 557 us, 128 643, errors 1.2e-6
-// and 6e-7 where plain products have 3.3e-6.)
+// accumulator: 4e-5 of the update).  fp32 updates therefore add the accumulators of 128 (pairs: 256) entries of the reduction in
+// registers.  Errors against 64 bits, of 49 x 1,270, 256 and 512 square by 128 entries 5e-7, 6e-7 and 6e-7, by 256 1.0e-6, 1.2e-6
+// and 1.1e-6 (five layers of 256 then 92 instead of 96 us), of 2,048 square by 256 1.2e-6, by 384 1.9e-6 (517 instead of 521 us);
+// plain fp32 products have 1.3e-6, 1.8e-6, 2.4e-6 and 3.6e-6.
+// APART: products with a lo part go to an accumulator of their own, so that one instruction multiplies a left hi part
+// with both parts of the right operand (four layers of 512 135 -> 128 us); the pairs, whose right operand is split over two
+// SMs, add them to the same one, a stage's small products first.
 template <int CTAS, int COLS, int NPROD> struct Cfg {
   static constexpr int M = CTAS * kRows, N = COLS;
   static constexpr int SUB = M / N;                       // tiles side by side in a square of M x M
   static constexpr int CHUNK = NPROD == 1 ? 1 << 30 : CTAS == 1 ? 2 : 4;
+  static constexpr bool APART = NPROD > 1 && CTAS == 1;
+  static constexpr int ACC = APART ? 2 * N : N;           // columns of an accumulator
   static constexpr int B_ROWS = N / CTAS;
   static constexpr int A_BYTES = kRows * kStep * 2, B_BYTES = B_ROWS * kStep * 2;
   static constexpr int PARTS = NPROD == 1 ? 1 : 2;        // hi; hi and lo
@@ -167,7 +172,7 @@ template <int CTAS, int COLS, int NPROD> struct Cfg {
   static constexpr int OFF_BAR = OFF_BLOCKS + STAGE_BYTES;
   static constexpr int OFF_TMEM = OFF_BAR + 8 * (2 * STAGES + 4 + kEpiWarps);
   static constexpr int SMEM_BYTES = OFF_TMEM + 16;
-  static constexpr int TMEM_COLS = 2 * N;
+  static constexpr int TMEM_COLS = 2 * ACC;
   static constexpr int WARP_COLS = N == 256 ? 64 : 32;    // of an epilogue warp
   static constexpr int WORKERS = 4 * (N / WARP_COLS);     // epilogue warps with something to do
   static_assert(SMEM_BYTES <= 227 * 1024 && M % N == 0 && WORKERS <= kEpiWarps, "shared memory of one SM, whole squares");
@@ -339,9 +344,9 @@ __device__ __forceinline__ void ask(const Maps& maps, const NsArgs& a, Pieces& w
     tma_load_3d<1>(w.hi + kBlockBytes, &maps.in_lo, col, row, z, w.bar);
   }
 }
-template <int MODE, bool TALL, int NPROD>
+template <int MODE, bool TALL, int NPROD, bool APART>
 __device__ __forceinline__ bool finish(const Maps& maps, const NsArgs& a, Pieces& w, const Tile& t, int row, int col,
-                                       uint32_t taddr) {
+                                       uint32_t taddr, int lo_cols) {
   if (row >= a.m || col >= a.n) return true;             // the whole warp
   const int lane = w.lane, r = lane >> 2, c = (lane & 3) * 2;
   const uint32_t lo_piece = w.hi + kBlockBytes;
@@ -367,7 +372,15 @@ __device__ __forceinline__ bool finish(const Maps& maps, const NsArgs& a, Pieces
   for (int h = 0; h < 2; ++h) {
     uint32_t v[16];
     tc_ld_blocks(taddr + (uint32_t(h * 16) << 16), v);
-    tc_wait_ld();
+    if (APART && lo_cols) {
+      uint32_t u[16];
+      tc_ld_blocks(taddr + lo_cols + (uint32_t(h * 16) << 16), u);
+      tc_wait_ld();
+#pragma unroll
+      for (int i = 0; i < 16; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) + __uint_as_float(u[i]));
+    } else {
+      tc_wait_ld();
+    }
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
       const int rb = 2 * h + s;
@@ -541,7 +554,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_ns_product(const __grid_constan
   const int kbegin = SPLIT ? all_ksteps * part / group : 0;
   const int ksteps = SPLIT ? all_ksteps * (part + 1) / group - kbegin : all_ksteps;
   enter();
-  // where SMs are free for the next launch's CTAs (five layers of 256: 100 -> 97 us)
+  // where SMs are free for the next launch's CTAs (3 us of five layers of 256)
   if (gridDim.x * 2 <= kNumSMs) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
   // Both of the next roles run with the whole warp, one lane of which issues: what the loops carry is then the same for all
@@ -580,6 +593,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_ns_product(const __grid_constan
       // fp32 accumulators, fp16 x fp16; bits 15 and 16: MN-major operands
       constexpr uint32_t idesc = (1u << 4) | (A_MN ? 1u << 15 : 0u) | (B_MN ? 1u << 16 : 0u) | (uint32_t(C::N >> 3) << 17) |
                                  (uint32_t(C::M >> 4) << 24);
+      constexpr uint32_t idesc_both = idesc + (uint32_t(C::N >> 3) << 17);       // twice the columns
       // a descriptor's address counts 16 bytes from its lowest bit
       const uint64_t a0 = operand_desc<A_MN>(base, 0), b0 = operand_desc<B_MN>(base + C::OFF_B, 0);
       constexpr int A_K = (A_MN ? 2048 : 32) >> 4, B_K = (B_MN ? 2048 : 32) >> 4, A_LO = C::A_BYTES >> 4, B_LO = C::B_BYTES >> 4;
@@ -590,23 +604,31 @@ __global__ void __launch_bounds__(kThreads, 1) k_ns_product(const __grid_constan
           const int k1 = k0 < ksteps - C::CHUNK ? k0 + C::CHUNK : ksteps, buf = lt & 1;
           if (lt > 1 && !wait_warp(bar_acc_empty(buf), ((lt >> 1) - 1) & 1)) { ok = false; break; }
           tc_fence_after();
-          const uint32_t acc = tmem_base + uint32_t(buf * C::N);
+          const uint32_t acc = tmem_base + uint32_t(buf * C::ACC);
           for (int k = k0; k < k1; ++k, ++it) {
             const int s = it % C::STAGES;
             if (!wait_warp(bar_full(s), (it / C::STAGES) & 1)) { ok = false; break; }
             tc_fence_after();
             const uint64_t da = a0 + uint64_t(s * (C::STAGE >> 4)), db = b0 + uint64_t(s * (C::STAGE >> 4));
             if (elected()) {
-              if (NPROD > 1) {
+              const uint32_t first = k > k0 ? 1u : 0u;
 #pragma unroll
-                for (int kk = 0; kk < kStep / 16; ++kk) {
-                  mma<CTAS>(acc, da + kk * A_K, db + kk * B_K + B_LO, idesc, k > k0 || kk ? 1u : 0u);
-                  mma<CTAS>(acc, da + kk * A_K + A_LO, db + kk * B_K, idesc, 1u);
+              for (int kk = 0; kk < kStep / 16; ++kk) {
+                const uint64_t ak = da + kk * A_K, bk = db + kk * B_K;
+                if (NPROD == 1) {
+                  mma<CTAS>(acc, ak, bk, idesc, first | kk ? 1u : 0u);
+                } else if (C::APART) {   // hi and lo of the right operand lie side by side, and so do the accumulator's halves
+                  mma<CTAS>(acc, ak, bk, idesc_both, first | kk ? 1u : 0u);
+                  mma<CTAS>(acc + C::N, ak + A_LO, bk, idesc, 1u);
+                } else {
+                  mma<CTAS>(acc, ak, bk + B_LO, idesc, first | kk ? 1u : 0u);
+                  mma<CTAS>(acc, ak + A_LO, bk, idesc, 1u);
                 }
               }
+              if (NPROD > 1 && !C::APART) {
 #pragma unroll
-              for (int kk = 0; kk < kStep / 16; ++kk)
-                mma<CTAS>(acc, da + kk * A_K, db + kk * B_K, idesc, NPROD > 1 || k > k0 || kk ? 1u : 0u);
+                for (int kk = 0; kk < kStep / 16; ++kk) mma<CTAS>(acc, da + kk * A_K, db + kk * B_K, idesc, 1u);
+              }
               commit<CTAS>(bar_empty(s));
               if (k + 1 == k1) commit<CTAS>(bar_acc_full(buf));
             }
@@ -636,13 +658,14 @@ __global__ void __launch_bounds__(kThreads, 1) k_ns_product(const __grid_constan
         for (int i = 0; i < 4 && !ok; ++i) ok = wait_warp(bar_acc_full(buf), (lt >> 1) & 1);
         if (!ok) break;
         tc_fence_after();
-        const uint32_t taddr = tmem_base + (uint32_t(q * 32) << 16) + uint32_t(buf * C::N + side * WC);
+        const uint32_t taddr = tmem_base + (uint32_t(q * 32) << 16) + uint32_t(buf * C::ACC + side * WC);
         if (NPROD > 1 && ksteps > C::CHUNK) {
           // the sums so far; with the last accumulator they go back into its place
-          uint32_t v[NPROD == 1 ? 1 : WC];
+          uint32_t v[NPROD == 1 ? 1 : WC], u[NPROD == 1 ? 1 : WC];
           if constexpr (NPROD > 1) {
             static_assert(WC == 32, "one load");
             tc_ld32(taddr, v);
+            if (C::APART) tc_ld32(taddr + C::N, u);
             tc_wait_ld();
           }
           if (k1 < ksteps) {             // the accumulator is free before its values are added
@@ -651,7 +674,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_ns_product(const __grid_constan
             if (lane == 0) arrive_first<CTAS>(bar_acc_empty(buf));
           }
 #pragma unroll
-          for (int i = 0; i < (NPROD == 1 ? 1 : WC); ++i) sum[i] = (k0 == 0 ? 0.f : sum[i]) + __uint_as_float(v[i]);
+          for (int i = 0; i < (NPROD == 1 ? 1 : WC); ++i) sum[i] = (k0 == 0 ? 0.f : sum[i]) + (C::APART ? __uint_as_float(v[i]) + __uint_as_float(u[i]) : __uint_as_float(v[i]));
           k0 = k1;
           if (k1 < ksteps) continue;
           if constexpr (NPROD > 1 && !SPLIT) {
@@ -667,7 +690,15 @@ __global__ void __launch_bounds__(kThreads, 1) k_ns_product(const __grid_constan
             for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(sum[NPROD == 1 ? 0 : i]);
           } else {
             tc_ld32(taddr, v);
-            tc_wait_ld();
+            if (C::APART) {
+              uint32_t u[32];
+              tc_ld32(taddr + C::N, u);
+              tc_wait_ld();
+#pragma unroll
+              for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) + __uint_as_float(u[i]));
+            } else {
+              tc_wait_ld();
+            }
           }
           uint8_t* to = smem + (q * 32 + lane) * kDumpPitch + side * 128;      // where the stages were: all are multiplied
 #pragma unroll
@@ -677,7 +708,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_ns_product(const __grid_constan
           for (int c = 0; ok && c < WC; c += 32) {
             if (c) ask<MODE>(maps, a, w, t.z, row, col + c);
             __syncwarp();
-            ok = finish<MODE, TALL, NPROD>(maps, a, w, t, row, col + c, taddr + c);
+            ok = finish<MODE, TALL, NPROD, C::APART>(maps, a, w, t, row, col + c, taddr + c, ksteps > C::CHUNK ? 0 : C::N);
           }
           tc_fence_before();
           __syncwarp();
@@ -724,7 +755,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_ns_product(const __grid_constan
       w.hi = base + C::OFF_BLOCKS + worker * 2 * kBlockBytes;
       w.bar = bar_in(worker);
       w.lane = lane;
-      finish<MODE, TALL, NPROD>(maps, a, w, t, t.row + q * 32, t.col + side * 32, taddr);
+      finish<MODE, TALL, NPROD, C::APART>(maps, a, w, t, t.row + q * 32, t.col + side * 32, taddr, 0);
       if (lane == 0) tma_wait_read<0>();
     }
     __syncwarp();
@@ -795,8 +826,9 @@ bool make_pieces(CUtensorMap* hi, CUtensorMap* lo, const Operand& o, int batch) 
   return make_map3(hi, o.p.hi, batch, o.rows, o.cols, o.ld, 32, true) && make_map3(lo, o.p.lo, batch, o.rows, o.cols, o.ld, 32, true);
 }
 
-// Tiles of a product: of 256 rows by a pair of CTAs where those keep most SMs busy, else of 128 x 128 (one product), else of
-// 128 x 64
+// Tiles of a product: of 256 rows by a pair of CTAs where those keep most SMs busy (4,096 square bf16 1,491 us, with tiles of
+// 128 x 128 1,990; but 1,001 square Gram matrices, 10 tiles of 256, by 72 of 128 x 64), else of 128 x 128 (one product), else of
+// 128 x 64 (five layers of 256 161 us in 128 x 128 when that was written, 118 in 128 x 64)
 template <int MODE, bool TALL, int NPROD>
 bool launch_product(const Operand& left, const Operand& right, const Operand* in, const Operand& out, const NsArgs& a, int batch,
                     cudaStream_t st) {
@@ -806,7 +838,7 @@ bool launch_product(const Operand& left, const Operand& right, const Operand* in
     const int64_t tm = (a.m + m - 1) / m, tn = (a.n + n - 1) / n;
     return (MODE == APPLY ? tm * tn : tm * (tm + 1) / 2 * (m / n)) * batch;
   };
-  const int kind = tiles(256, WIDE) >= 60 ? 2 : NPROD == 1 && tiles(128, 128) >= 100 ? 1 : 0;
+  const int kind = tiles(256, WIDE) >= 60 && a.m > 128 && a.n > 128 ? 2 : NPROD == 1 && tiles(128, 128) >= 100 && a.n > 64 ? 1 : 0;
   const int outer = kind == 2 ? WIDE / 2 : kind == 1 ? 128 : 64;
   Maps maps;
   if (!make_operand(&maps.a_hi, &maps.a_lo, left, batch, A_MN, kRows, NPROD > 1) ||

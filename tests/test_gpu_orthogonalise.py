@@ -76,13 +76,17 @@ def test_many_steps_stay_where_the_quintic_keeps_them(dtype):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
-@pytest.mark.parametrize("shape", [(5, 256, 256), (7, 65, 70), (3, 700, 90), (2, 1, 1), (40, 32, 48)])
+@pytest.mark.parametrize("shape", [(5, 256, 256), (7, 65, 70), (3, 700, 90), (2, 1, 1), (40, 32, 48), (45, 200, 150)])
 def test_batches_are_their_matrices(dtype, shape):
     g = make(dtype, *shape, seed=1)
     got = xrl.xrl_orthogonalise(g)
     assert off(got, define(g)) <= TOL[dtype]
     for z in range(shape[0]):
-        assert torch.equal(xrl.xrl_orthogonalise(g[z]), got[z])
+        # alone a matrix may be cut into other tiles, whose sums are added in another order
+        alone = xrl.xrl_orthogonalise(g[z])
+        assert off(alone, got[z].double()) <= 2 * TOL[dtype]
+        same = xrl.xrl_orthogonalise(g[z][None].expand(shape[0], -1, -1).contiguous())
+        assert torch.equal(same[z], got[z])                       # but not by what the others hold
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
