@@ -418,9 +418,9 @@ __device__ __forceinline__ float remote_f(uint32_t at) {
   asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
   return v;
 }
-__device__ __forceinline__ int32_t remote_i(uint32_t at) {
-  int32_t v;
-  asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
+__device__ __forceinline__ uint64_t remote_u64(uint32_t at) {
+  uint64_t v;
+  asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(at) : "memory");
   return v;
 }
 
@@ -478,24 +478,32 @@ __device__ __forceinline__ void add_chunk(Sums& q, const uint4 (&v)[U], float c,
 }
 
 // ---- the best k of a CTA's part of a row -----------------------------------------------------------------------
+// An entry as one whole number: by value first, the lower index then; 0 is none
+__device__ __forceinline__ uint64_t rank_key(float v, int32_t i) { return uint64_t(key_of(v)) << 32 | uint32_t(~i); }
+__device__ __forceinline__ Best best_of(uint64_t key) {
+  Best b;
+  if (key) { b.v = float_of(uint32_t(key >> 32)); b.i = int32_t(~uint32_t(key)); }
+  return b;
+}
 // Candidates in shared memory: the k best of n <= THREADS, by counting for each how many are better
 template <int THREADS> struct Candidates {
-  float v[THREADS];
-  int32_t i[THREADS];
-  float best_v[kMostTop];
-  int32_t best_i[kMostTop];
+  uint64_t key[THREADS], best[kMostTop];
   uint8_t flagged[THREADS];              // of each warp: the lanes that are walked again
   int n;
 };
 template <int THREADS> __device__ __forceinline__ void rank_candidates(Candidates<THREADS>& s, int n, int k) {
-  if (threadIdx.x < kMostTop) { s.best_v[threadIdx.x] = kNegInf; s.best_i[threadIdx.x] = INT32_MAX; }
+  if (threadIdx.x < kMostTop) s.best[threadIdx.x] = 0;
+  if (int(threadIdx.x) >= n) s.key[threadIdx.x] = 0;
   __syncthreads();
   if (int(threadIdx.x) < n) {
-    const float v = s.v[threadIdx.x];
-    const int32_t i = s.i[threadIdx.x];
+    const uint64_t mine = s.key[threadIdx.x];
     int rank = 0;
-    for (int j = 0; j < n; ++j) rank += better(s.v[j], s.i[j], v, i) ? 1 : 0;
-    if (rank < k && v > kNegInf) { s.best_v[rank] = v; s.best_i[rank] = i; }
+#pragma unroll 4
+    for (int j = 0; j < n; j += 2) {
+      const ulonglong2 two = *reinterpret_cast<const ulonglong2*>(&s.key[j]);
+      rank += (two.x > mine ? 1 : 0) + (two.y > mine ? 1 : 0);
+    }
+    if (rank < k && mine) s.best[rank] = mine;
   }
   __syncthreads();
 }
@@ -537,7 +545,7 @@ __device__ __forceinline__ void best_of_part(const Row<T>& r, int v0, int v1, bo
   auto put = [&](float v, int32_t i) {
     if (v >= bound && v > kNegInf) {
       const int at = atomicAdd(&s.n, 1);
-      if (at < THREADS) { s.v[at] = v; s.i[at] = i; }
+      if (at < THREADS) s.key[at] = rank_key(v, i);
     }
   };
   for (int i = lane; i < items; i += 32) {
@@ -577,8 +585,7 @@ __device__ __forceinline__ void best_of_part(const Row<T>& r, int v0, int v1, bo
       const int j = lane < 16 ? r.edge(lane) : -1;
       offer(mine_b, last, j >= 0 ? r.at(j) : kNegInf, j, k, lane);
     }
-    s.v[threadIdx.x] = mine_b.v;
-    s.i[threadIdx.x] = mine_b.i;
+    s.key[threadIdx.x] = mine_b.v > kNegInf ? rank_key(mine_b.v, mine_b.i) : 0;
     __syncthreads();
     n = THREADS;
   }
@@ -593,7 +600,7 @@ __global__ void __launch_bounds__(THREADS, CTAS) k_logprob_cta(RowArgs a, RowOut
   constexpr int N = Vec<T>::N, W = THREADS / 32, GROUP = U * THREADS;
   __shared__ Sums s_sums[W];
   __shared__ float s_red[64];
-  __shared__ Candidates<TOP ? THREADS : 32> s_best;
+  __shared__ __align__(16) Candidates<TOP ? THREADS : 32> s_best;
   __shared__ Sums s_part;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int parts = 1 << log_parts, part = parts > 1 ? int(cluster_rank()) : 0;
@@ -659,27 +666,20 @@ __global__ void __launch_bounds__(THREADS, CTAS) k_logprob_cta(RowArgs a, RowOut
       largest = max_warp(q.m);
       q = join_warp(q);
       if (TOP) {
-        const int p = threadIdx.x / kMostTop, e = threadIdx.x % kMostTop;
-        float v = kNegInf;
-        int32_t i = INT32_MAX;
-        if (p < parts) {
-          v = remote_f(remote(&s_best.best_v[e], p));
-          i = remote_i(remote(&s_best.best_i[e], p));
-        }
-        s_best.v[threadIdx.x] = v;
-        s_best.i[threadIdx.x] = i;
+        const int p = threadIdx.x / o.top, e = threadIdx.x - p * o.top;
+        s_best.key[threadIdx.x] = p < parts ? remote_u64(remote(&s_best.best[e], p)) : 0;
       }
     }
     cluster_arrive_wait();               // nobody leaves, and nothing is written again, while it is read
     if (part != 0) return;
-    if (TOP) rank_candidates(s_best, parts * kMostTop, o.top);
+    if (TOP) rank_candidates(s_best, parts * o.top, o.top);
   }
   if (largest > kNegInf && largest < INFINITY && !(largest * c > kLow && largest * c < kHigh)) {       // (all threads agree)
     careful_row<T, THREADS>(a, MASK, row, s_red, q);
     if (warp == 0) {
       const RowNorm n = {q.m, kLn2 * log2f(q.s)};
       if (lane == 0) write_row(a, o, row, given, n, entropy_of(q));
-      if (TOP) write_top(a, o, row, n, Best{s_best.best_v[lane], s_best.best_i[lane]}, lane);
+      if (TOP) write_top(a, o, row, n, best_of(s_best.best[lane]), lane);
     }
   } else if (warp == 0) {
     RowNorm n = {kNegInf, kNegInf};
@@ -690,7 +690,7 @@ __global__ void __launch_bounds__(THREADS, CTAS) k_logprob_cta(RowArgs a, RowOut
       entropy = entropy_of(q);
     }
     if (lane == 0) write_row(a, o, row, given, n, entropy);
-    if (TOP) write_top(a, o, row, n, Best{s_best.best_v[lane], s_best.best_i[lane]}, lane);
+    if (TOP) write_top(a, o, row, n, best_of(s_best.best[lane]), lane);
   }
 }
 
