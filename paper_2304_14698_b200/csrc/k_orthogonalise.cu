@@ -329,6 +329,7 @@ struct Maps { CUtensorMap a_hi, a_lo, b_hi, b_lo, in_hi, in_lo, out_hi, out_lo; 
 // result will be; the result goes through shared memory to the TMA unit, and its transpose after it.
 struct Pieces {
   uint32_t hi, bar;                      // lo: kBlockBytes behind hi
+  uint32_t turned;                       // where the transpose leaves from: a place of its own where half the warps are idle, or hi
   uint32_t phase = 0;
   int lane;
 };
@@ -475,18 +476,20 @@ __device__ __forceinline__ bool finish(const Maps& maps, const NsArgs& a, Pieces
     tma_commit();
   }
   if (MODE != APPLY && t.turned) {                       // below the diagonal
-    if (lane == 0) tma_wait_read<0>();
-    __syncwarp();
+    if (w.turned == w.hi) {
+      if (lane == 0) tma_wait_read<0>();
+      __syncwarp();
+    }
 #pragma unroll
     for (int rb = 0; rb < 4; ++rb) {
-      stmatrix4<true>(block_at(w.hi, lane, rb), hi[rb]);
-      if (LO) stmatrix4<true>(block_at(lo_piece, lane, rb), lo[rb]);
+      stmatrix4<true>(block_at(w.turned, lane, rb), hi[rb]);
+      if (LO) stmatrix4<true>(block_at(w.turned + kBlockBytes, lane, rb), lo[rb]);
     }
     fence_async_smem();
     __syncwarp();
     if (lane == 0) {
-      tma_store_3d(&maps.out_hi, w.hi, row, col, t.z);
-      if (LO) tma_store_3d(&maps.out_lo, lo_piece, row, col, t.z);
+      tma_store_3d(&maps.out_hi, w.turned, row, col, t.z);
+      if (LO) tma_store_3d(&maps.out_lo, w.turned + kBlockBytes, row, col, t.z);
       tma_commit();
     }
   }
@@ -497,11 +500,9 @@ __device__ __forceinline__ void prefetch_map(const CUtensorMap* m) {
   asm volatile("prefetch.tensormap [%0];" ::"l"(m) : "memory");
 }
 
-constexpr int kDumpPitch = 68 * 4;       // bytes of a row of a tile's 64 fp32 columns
-
 // SPLIT: a cluster of up to eight CTAs shares a tile of a long reduction, a stretch of it each; the accumulators then meet
-// through the cluster's shared memory, each CTA adding up (always in the same order) and finishing some of the tile's eight
-// pieces.  For Gram matrices of few tiles.
+// through the cluster's shared memory, each CTA adding up (always in the same order) and finishing some of the tile's pieces.  For
+// Gram matrices of few tiles.
 template <int CTAS, int COLS, int MODE, bool TALL, int NPROD, bool SPLIT>
 __global__ void __launch_bounds__(kThreads, 1) k_ns_product(const __grid_constant__ Maps maps, const NsArgs a) {
   using C = Cfg<CTAS, COLS, NPROD>;
@@ -509,6 +510,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_ns_product(const __grid_constan
   extern __shared__ __align__(1024) uint8_t smem[];
   const uint32_t base = smem_u32(smem);
   const int warp = __shfl_sync(0xFFFFFFFFu, int(threadIdx.x) >> 5, 0), lane = threadIdx.x & 31;
+  constexpr int DUMP = (C::N + 4) * 4;   // bytes of a row of a tile in shared memory
   const int group = SPLIT ? a.parts : CTAS;
   const int rank = SPLIT ? 0 : int(blockIdx.x) % CTAS, part = SPLIT ? int(blockIdx.x) % group : 0;
   const int first = int(blockIdx.x) / group, step = int(gridDim.x) / group;
@@ -643,6 +645,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_ns_product(const __grid_constan
     const int q = warp & 3, side = (warp - 2) >> 2;
     Pieces w;
     w.hi = base + C::OFF_BLOCKS + (warp - 2) * 2 * kBlockBytes;
+    w.turned = w.hi + (2 * C::WORKERS <= kEpiWarps ? C::WORKERS * 2 * kBlockBytes : 0);
     w.bar = bar_in(warp - 2);
     w.lane = lane;
     uint32_t lt = 0;
@@ -700,7 +703,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_ns_product(const __grid_constan
               tc_wait_ld();
             }
           }
-          uint8_t* to = smem + (q * 32 + lane) * kDumpPitch + side * 128;      // where the stages were: all are multiplied
+          uint8_t* to = smem + (q * 32 + lane) * DUMP + side * 128;      // where the stages were: all are multiplied
 #pragma unroll
           for (int i = 0; i < 32; i += 4) *reinterpret_cast<uint4*>(to + 4 * i) = make_uint4(v[i], v[i + 1], v[i + 2], v[i + 3]);
         } else {
@@ -726,11 +729,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_ns_product(const __grid_constan
   if constexpr (SPLIT) {
     __syncwarp();
     tile_sync<2>();
-    const int share = 8 / group, worker = warp - 2;
+    const int share = C::WORKERS / group, worker = warp - 2;
     if (worker >= 0 && worker < share && first < total) {
       const Tile t = tile_of<C::M, C::N, SYM>(a, first);
       const int piece = part * share + worker, q = piece & 3, side = piece >> 2;
-      const uint32_t from = base + (q * 32 + lane) * kDumpPitch + side * 128;
+      const uint32_t from = base + (q * 32 + lane) * DUMP + side * 128;
       float sum[32];
 #pragma unroll
       for (int i = 0; i < 32; ++i) sum[i] = 0.f;
@@ -747,12 +750,14 @@ __global__ void __launch_bounds__(kThreads, 1) k_ns_product(const __grid_constan
         }
       }
       tc_fence_after();
-      const uint32_t taddr = tmem_base + (uint32_t((warp & 3) * 32) << 16);    // as a place to turn rows into 8 x 8 blocks
+      // as a place to turn rows into 8 x 8 blocks: 32 columns for each of the warps that share 32 lanes
+      const uint32_t taddr = tmem_base + (uint32_t((warp & 3) * 32) << 16) + uint32_t(worker >> 2) * 32;
       tc_st16(taddr, sum);
       tc_st16(taddr + 16, sum + 16);
       asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
       Pieces w;
       w.hi = base + C::OFF_BLOCKS + worker * 2 * kBlockBytes;
+      w.turned = w.hi + share * 2 * kBlockBytes;         // (half the workers at most have a piece)
       w.bar = bar_in(worker);
       w.lane = lane;
       finish<MODE, TALL, NPROD, C::APART>(maps, a, w, t, t.row + q * 32, t.col + side * 32, taddr, 0);
@@ -838,8 +843,25 @@ bool launch_product(const Operand& left, const Operand& right, const Operand* in
     const int64_t tm = (a.m + m - 1) / m, tn = (a.n + n - 1) / n;
     return (MODE == APPLY ? tm * tn : tm * (tm + 1) / 2 * (m / n)) * batch;
   };
-  const int kind = tiles(256, WIDE) >= 60 && a.m > 128 && a.n > 128 ? 2 : NPROD == 1 && tiles(128, 128) >= 100 && a.n > 64 ? 1 : 0;
-  const int outer = kind == 2 ? WIDE / 2 : kind == 1 ? 128 : 64;
+  // (where a pair has less than two tiles of a short reduction to apply, smaller ones let one's epilogue run under the next one's
+  // products: 4,100 x 1,001 209 -> 203 us, 1,024 x 4,096 183 -> 179; but 2,048 square 238 -> 244, 2,800 450 -> 503)
+  const bool shallow = MODE == APPLY && NPROD == 1 && a.k <= 1024 && tiles(256, WIDE) < kNumSMs && tiles(128, 128) > kNumSMs;
+  const int kind = !shallow && tiles(256, WIDE) >= 60 && a.m > 128 && a.n > 128 ? 2
+                   : NPROD == 1 && tiles(128, 128) >= 100 && a.n > 64 ? 1 : 0;
+  // A long reduction of few tiles: one tile to a cluster, and shares that are worth the meeting, some 3 us: 12 stages of one
+  // product or 5 of three (fp32 49 x 1,270 109 -> 100 us, bf16 4,100 x 1,001 228 -> 209; but fp32 256 x 512 in two 107 -> 111, bf16
+  // 128 x 1,024 in four 70 -> 84).  Clusters of two, four and eight have room for 72, 32 and 16 on the GPU at a time (36 clusters of
+  // four: 4,100 x 1,001 209 -> 306).  A stage of 128 columns takes 512 cycles, of 64 375; one product has either.
+  const int stages = (a.k + kStep - 1) / kStep;
+  auto shares = [&](int columns) {
+    int p = 1;
+    while (p < 8 && tiles(128, columns) <= (p == 1 ? 72 : p == 2 ? 32 : 16) && stages >= (NPROD == 1 ? 24 : 10) * p) p *= 2;
+    return p;
+  };
+  const bool shared = MODE == GRAM && kind == 0;
+  const int parts64 = shared ? shares(64) : 1, parts128 = shared && NPROD == 1 ? shares(128) : 1;
+  const bool wide = parts128 > 1 && 512 * parts64 < 375 * parts128;
+  const int outer = kind == 2 ? WIDE / 2 : kind == 1 || wide ? 128 : 64;
   Maps maps;
   if (!make_operand(&maps.a_hi, &maps.a_lo, left, batch, A_MN, kRows, NPROD > 1) ||
       !make_operand(&maps.b_hi, &maps.b_lo, right, batch, B_MN, outer, NPROD > 1) ||
@@ -848,13 +870,10 @@ bool launch_product(const Operand& left, const Operand& right, const Operand* in
   if (kind == 2) return launch_tiles<2, WIDE, MODE, TALL, NPROD>(maps, a, batch, st);
   if (NPROD == 1 && kind == 1) return launch_tiles<1, NPROD == 1 ? 128 : 64, MODE, TALL, NPROD>(maps, a, batch, st);
   if constexpr (MODE == GRAM) {
-    // One tile to a cluster, and shares that are worth the meeting, some 3 us: 12 stages of one product or 5 of three
-    // (fp32 49 x 1,270 109 -> 100 us, bf16 4,100 x 1,001 228 -> 209; but fp32 256 x 512 in two 107 -> 111, bf16 128 x 1,024 in
-    // four 70 -> 84).
-    int parts = 1;
-    while (parts < 8 && tiles(128, 64) * parts * 2 <= kNumSMs && (a.k + kStep - 1) / kStep >= (NPROD == 1 ? 24 : 10) * parts)
-      parts *= 2;
-    if (parts > 1) return launch_tiles<1, 64, MODE, TALL, NPROD, true>(maps, a, batch, st, parts);
+    if constexpr (NPROD == 1) {
+      if (wide) return launch_tiles<1, 128, MODE, TALL, NPROD, true>(maps, a, batch, st, parts128);
+    }
+    if (parts64 > 1) return launch_tiles<1, 64, MODE, TALL, NPROD, true>(maps, a, batch, st, parts64);
   }
   return launch_tiles<1, 64, MODE, TALL, NPROD>(maps, a, batch, st);
 }

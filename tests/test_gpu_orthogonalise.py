@@ -176,7 +176,7 @@ def test_empty_batches():
 
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("shape", [(1, 16, 4000), (1, 4000, 16), (3, 130, 2100), (1, 2100, 130), (1, 500, 1111), (1, 100, 513), (8, 64, 900),
-                                   (1, 60, 32768), (1, 1, 5000)])
+                                   (1, 60, 32768), (1, 1, 5000), (1, 700, 3500), (1, 3500, 650), (1, 400, 7000), (1, 7000, 390)])
 def test_long_reductions_are_shared_out(dtype, shape):
     for kind in ("gradient", "normal"):
         g = make(dtype, *shape, seed=shape[1], kind=kind)
