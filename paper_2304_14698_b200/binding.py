@@ -389,9 +389,12 @@ def _flat(where, what, t, dtype, shape):
 
 def _rows_of(where, what, t, rows, vocab):
     """(pointer, row stride) of a [rows x vocab] tensor whose rows may lie apart."""
-    if t.shape != (rows, vocab) or (vocab > 1 and t.stride(1) != 1):
-        raise XrlError(1, f"{where} ({what}: [{rows} x {vocab}], entries of a row side by side)")
-    return t.data_ptr(), t.stride(0) if rows > 1 else vocab
+    if t.shape != (rows, vocab):
+        raise XrlError(1, f"{where} ({what}: [{rows} x {vocab}])")
+    row, entry = t.stride()
+    if entry != 1 and vocab > 1:
+        raise XrlError(1, f"{where} ({what}: entries of a row side by side)")
+    return t.data_ptr(), row if rows > 1 else vocab
 
 
 def _mask_of(where, mask, rows, vocab):
@@ -400,6 +403,8 @@ def _mask_of(where, mask, rows, vocab):
         return None, 0
     if (mask.dtype is not _th().uint8 and mask.dtype is not _th().bool) or mask.dim() not in (1, 2):
         raise XrlError(1, f"{where} (mask: uint8 or bool, [rows x vocab], [1 x vocab] or [vocab])")
+    if mask.shape == (rows, vocab):
+        return _rows_of(where, "mask", mask, rows, vocab)
     one = mask.dim() == 1 or (mask.shape[0] == 1 and rows != 1)
     ptr, stride = _rows_of(where, "mask", mask if mask.dim() == 2 else mask[None], 1 if one else rows, vocab)
     return ptr, 0 if one else stride
@@ -416,37 +421,41 @@ def xrl_logprob(logits, token=None, mask=None, scale=1.0, top=0, out=None, strea
     if stream is not None and out is None and logits.is_cuda:
         with _stream_scope(stream, logits.device):
             return xrl_logprob(logits, token, mask, scale, top)
-    if logits.dim() != 2:
+    shape = logits.shape
+    if len(shape) != 2:
         raise XrlError(1, f"{where} (logits: [rows x vocab])")
-    rows, vocab = logits.shape
+    rows, vocab = shape
     f32 = th.float32
+    dev = _device_of(where, logits, token, mask)
+    dtype = _storage(where, logits)
+    x, stride = _rows_of(where, "logits", logits, rows, vocab)
+    tp = None if token is None else _flat(where, "token", token, th.int32, (rows,))
+    mp, mstride = (None, 0) if mask is None else _mask_of(where, mask, rows, vocab)
+    lp = tt = tl = None
     if out is None:
-        dev = _device_of(where, logits, token, mask)
         entropy = th.empty(rows, dtype=f32, device=logits.device)
         norm = entropy.new_empty((rows, 2))
         o = {"entropy": entropy, "norm": norm}
-        ep, np_, lp, tt, tl = entropy.data_ptr(), norm.data_ptr(), None, None, None
+        ep, np_ = entropy.data_ptr(), norm.data_ptr()
         if token is not None:
             o["logp"] = logp = entropy.new_empty(rows)
             lp = logp.data_ptr()
         if top > 0:
-            o["top_token"] = a = entropy.new_empty((rows, top), dtype=th.int32)
+            o["top_token"] = a = th.empty((rows, top), dtype=th.int32, device=logits.device)
             o["top_logp"] = b = entropy.new_empty((rows, top))
             tt, tl = a.data_ptr(), b.data_ptr()
     else:
         o = out
-        dev = _device_of(where, logits, token, mask, *o.values())
+        _device_of(where, logits, *o.values())
         ep = _flat(where, "entropy", o.get("entropy"), f32, (rows,))
         np_ = _flat(where, "norm", o.get("norm"), f32, (rows, 2))
         lp = _flat(where, "logp", o.get("logp"), f32, (rows,))
         tt = _flat(where, "top_token", o.get("top_token"), th.int32, (rows, top))
         tl = _flat(where, "top_logp", o.get("top_logp"), f32, (rows, top))
-    x, stride = _rows_of(where, "logits", logits, rows, vocab)
-    mp, mstride = _mask_of(where, mask, rows, vocab)
-    st = load_library().xrl_logprob(dev, _storage(where, logits), rows, vocab, x, stride,
-                                    _flat(where, "token", token, th.int32, (rows,)), mp, mstride, scale, top, lp, ep, np_, tt, tl,
-                                    _stream_on(dev, stream))
-    _check(st, where)
+    st = (_lib or load_library()).xrl_logprob(dev, dtype, rows, vocab, x, stride, tp, mp, mstride, scale, top, lp, ep, np_, tt, tl,
+                                              _stream_on(dev, stream))
+    if st:
+        raise XrlError(st, where)
     return o
 
 
@@ -460,9 +469,10 @@ def xrl_logprob_grad(logits, norm, token=None, dlogp=None, entropy=None, dentrop
     if stream is not None and grad is None and logits.is_cuda:
         with _stream_scope(stream, logits.device):
             return xrl_logprob_grad(logits, norm, token, dlogp, entropy, dentropy, mask, scale)
-    if logits.dim() != 2:
+    shape = logits.shape
+    if len(shape) != 2:
         raise XrlError(1, f"{where} (logits: [rows x vocab])")
-    rows, vocab = logits.shape
+    rows, vocab = shape
     f32, each = th.float32, (rows,)
     dev = _device_of(where, logits, norm, token, dlogp, entropy, dentropy, mask, grad)
     dtype = _storage(where, logits)
@@ -472,13 +482,14 @@ def xrl_logprob_grad(logits, norm, token=None, dlogp=None, entropy=None, dentrop
         raise XrlError(1, f"{where} (grad: the type of the logits)")
     x, stride = _rows_of(where, "logits", logits, rows, vocab)
     gp, gstride = _rows_of(where, "grad", grad, rows, vocab)
-    mp, mstride = _mask_of(where, mask, rows, vocab)
-    st = load_library().xrl_logprob_grad(
+    mp, mstride = (None, 0) if mask is None else _mask_of(where, mask, rows, vocab)
+    st = (_lib or load_library()).xrl_logprob_grad(
         dev, dtype, rows, vocab, x, stride, _flat(where, "token", token, th.int32, each), mp, mstride, scale,
         _flat(where, "norm", norm, f32, (rows, 2)), _flat(where, "dlogp", dlogp, f32, each),
         _flat(where, "entropy", entropy, f32, each), _flat(where, "dentropy", dentropy, f32, each), gp, gstride,
         _stream_on(dev, stream))
-    _check(st, where)
+    if st:
+        raise XrlError(st, where)
     return grad
 
 
