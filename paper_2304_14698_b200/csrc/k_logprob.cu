@@ -450,12 +450,12 @@ __device__ __forceinline__ float spread(const uint4 (&v)[U], f32x2 (&f)[U * 2], 
     f[i] = pair(max_nan(__uint_as_float(w[2 * i]), floor), max_nan(__uint_as_float(w[2 * i + 1]), floor));
   return m;
 }
-// adds them to a thread's sums
+// adds them to a thread's sums; the largest of them
 template <typename T, int U>
-__device__ __forceinline__ void add_chunk(Sums& q, const uint4 (&v)[U], float c, float floor) {
+__device__ __forceinline__ float add_chunk(Sums& q, const uint4 (&v)[U], float c, float floor) {
   constexpr int P = U * Vec<T>::N / 2;
   f32x2 f[P];
-  const float m = fmaxf(q.m, spread<U>(v, f, floor, static_cast<const T*>(nullptr)));
+  const float here = spread<U>(v, f, floor, static_cast<const T*>(nullptr)), m = fmaxf(q.m, here);
   const float r = fmaxf(m, floor) * c, d = q.r - r, e = ex2(d);
   const f32x2 cc = pair(c, c), rr = pair(-r, -r);
   f32x2 s[2] = {pair(q.s * e, 0.f), 0ull}, t[2] = {pair(fmaf(d, q.s, q.t) * e, 0.f), 0ull};
@@ -475,6 +475,7 @@ __device__ __forceinline__ void add_chunk(Sums& q, const uint4 (&v)[U], float c,
   q.t = a + b;
   q.m = m;
   q.r = r;
+  return here;
 }
 
 // ---- the best k of a CTA's part of a row -----------------------------------------------------------------------
@@ -485,10 +486,12 @@ __device__ __forceinline__ Best best_of(uint64_t key) {
   if (key) { b.v = float_of(uint32_t(key >> 32)); b.i = int32_t(~uint32_t(key)); }
   return b;
 }
+constexpr int kSlots = 8;                // stretches of a thread's vectors
 // Candidates in shared memory: the k best of n <= THREADS, by counting for each how many are better
 template <int THREADS> struct Candidates {
   uint64_t key[THREADS], best[kMostTop];
-  uint8_t flagged[THREADS];              // of each warp: the lanes that are walked again
+  float largest[kSlots][THREADS];        // of each stretch of each thread's vectors
+  uint8_t again[kSlots * THREADS];       // of each warp: lane and stretch (times 32) of what is walked again
   int n;
 };
 template <int THREADS> __device__ __forceinline__ void rank_candidates(Candidates<THREADS>& s, int n, int k) {
@@ -508,12 +511,13 @@ template <int THREADS> __device__ __forceinline__ void rank_candidates(Candidate
   __syncthreads();
 }
 
-// A thread's largest logit (thread_max) is known.  At least k threads hold one of `bound` or more, so the k best are no
-// less; few other logits are, and only the threads whose largest is that high have any.  Their vectors are read again, spread
-// over the lanes of their warp, and what reaches the bound is ranked.  Where that is more than one entry per thread of
-// the CTA (equal logits everywhere, or fewer than k threads with any) each warp keeps a sorted list of its whole part instead.
+// A thread's largest logit (thread_max) is known, and that of each of up to eight stretches of its vectors, `stretch` vectors
+// long.  At least k threads hold one of `bound` or more, so the k best are no less; few other logits are, and only the
+// stretches whose largest is that high have any.  Their vectors are read again, spread over the lanes of their warp, and what
+// reaches the bound is ranked.  Where that is more than one entry per thread of the CTA (equal logits everywhere, or fewer than
+// k threads with any) each warp keeps a sorted list of its whole part instead.
 template <typename T, int THREADS, bool MASK>
-__device__ __forceinline__ void best_of_part(const Row<T>& r, int v0, int v1, bool edges, float thread_max, float part_max, int k,
+__device__ __forceinline__ void best_of_part(const Row<T>& r, int v0, int v1, bool edges, float thread_max, float part_max, int stretches, int stretch, int k,
                                              Candidates<THREADS>& s, uint32_t* red) {
   constexpr int N = Vec<T>::N, U = 4, W = THREADS / 32, GROUP = THREADS / 32;
   static_assert(GROUP <= 32, "32 groups of threads");
@@ -538,10 +542,19 @@ __device__ __forceinline__ void best_of_part(const Row<T>& r, int v0, int v1, bo
     }
   }
   const float bound = float_of(lo);
-  const unsigned flags = __ballot_sync(kAll, thread_max > kNegInf && mine >= lo);
-  const int iters = (v1 - v0 + THREADS - 1) / THREADS, items = __popc(flags) * iters;
-  if (flags >> lane & 1) s.flagged[warp * 32 + __popc(flags & ((1u << lane) - 1))] = uint8_t(lane);
-  __syncwarp();
+  uint8_t* again = s.again + warp * 32 * kSlots;
+  int items = 0;
+  if (__any_sync(kAll, thread_max > kNegInf && mine >= lo)) {
+    for (int i = 0; i < stretches; ++i) {
+      const float most = s.largest[i][threadIdx.x];
+      const bool some = most > kNegInf && most >= bound;
+      const unsigned flags = __ballot_sync(kAll, some);
+      if (some) again[items + __popc(flags & ((1u << lane) - 1))] = uint8_t(i * 32 + lane);
+      items += __popc(flags);
+    }
+    items *= stretch;
+    __syncwarp();
+  }
   auto put = [&](float v, int32_t i) {
     if (v >= bound && v > kNegInf) {
       const int at = atomicAdd(&s.n, 1);
@@ -549,7 +562,8 @@ __device__ __forceinline__ void best_of_part(const Row<T>& r, int v0, int v1, bo
     }
   };
   for (int i = lane; i < items; i += 32) {
-    const int j = v0 + warp * 32 + s.flagged[warp * 32 + i / iters] + (i % iters) * THREADS;
+    const int which = i / stretch, at = again[which];
+    const int j = v0 + warp * 32 + (at & 31) + ((at >> 5) * stretch + i - which * stretch) * THREADS;
     if (j < v1) {
       const uint4 v = r.template vec<MASK>(j);
       float f[N];
@@ -618,26 +632,40 @@ __global__ void __launch_bounds__(THREADS, CTAS) k_logprob_cta(RowArgs a, RowOut
   const int v0 = start_of(r.vecs, part), v1 = start_of(r.vecs, part + 1);
   Sums q = zero;
   int j = v0 + threadIdx.x;              // the thread's next vector
+  // the largest of a stretch of `rounds` of the loop
+  const int rounds = TOP ? max((v1 - v0 + kSlots * GROUP - 1) / (kSlots * GROUP), 1) : 1;
+  float most = kNegInf;
+  int round = 0, slot = 0;
   for (int left = v1 - v0; left > 0; left -= GROUP, j += GROUP) {
+    float here = kNegInf;
     if (left >= GROUP) {
       uint4 v[U];
 #pragma unroll
       for (int u = 0; u < U; ++u) v[u] = r.template vec<MASK>(j + u * THREADS);
-      add_chunk<T, U>(q, v, c, floor);
+      here = add_chunk<T, U>(q, v, c, floor);
     } else if (2 * left > GROUP) {
       uint4 v[U];
 #pragma unroll
       for (int u = 0; u < U; ++u) v[u] = j + u * THREADS < v1 ? r.template vec<MASK>(j + u * THREADS) : Vec<T>::none();
-      add_chunk<T, U>(q, v, c, floor);
+      here = add_chunk<T, U>(q, v, c, floor);
     } else {
 #pragma unroll 1
       for (int u = 0; u < U; ++u) {
         if (j + u * THREADS - lane >= v1) break;         // no vector for the whole warp
         const uint4 v[1] = {j + u * THREADS < v1 ? r.template vec<MASK>(j + u * THREADS) : Vec<T>::none()};
-        add_chunk<T, 1>(q, v, c, floor);
+        here = fmaxf(here, add_chunk<T, 1>(q, v, c, floor));
+      }
+    }
+    if (TOP) {
+      most = fmaxf(most, here);
+      if (++round == rounds) {
+        s_best.largest[slot++][threadIdx.x] = most;
+        most = kNegInf;
+        round = 0;
       }
     }
   }
+  if (TOP && round) s_best.largest[slot++][threadIdx.x] = most;
   const float thread_max = q.m;          // (of its whole vectors)
   if (part == 0 && threadIdx.x < 16) {
     const int j = r.edge(threadIdx.x);
@@ -651,7 +679,8 @@ __global__ void __launch_bounds__(THREADS, CTAS) k_logprob_cta(RowArgs a, RowOut
   __syncthreads();
   q = lane < W ? s_sums[lane] : zero;
   float largest = max_warp(q.m);
-  if (TOP) best_of_part<T, TOP ? THREADS : 32, MASK>(r, v0, v1, part == 0, thread_max, largest, o.top, s_best, reinterpret_cast<uint32_t*>(s_red));
+  if (TOP) best_of_part<T, TOP ? THREADS : 32, MASK>(r, v0, v1, part == 0, thread_max, largest, slot,
+                                                         min(rounds * U, (v1 - v0 + THREADS - 1) / THREADS), o.top, s_best, reinterpret_cast<uint32_t*>(s_red));
   if (parts > 1 || warp == 0) q = join_warp(q);
   if (parts > 1) {
     if (threadIdx.x == 0) s_part = q;
@@ -970,8 +999,10 @@ void launch_cta(const RowArgs& a, const RowOut& o, int log_parts, cudaStream_t s
 }
 // Threads, vectors a thread has in flight, CTAs an SM holds.  Measured in us, 16,384 rows of 1,200 and 8,000, 8,192 of 32,000, bf16:
 // 64 threads by four vectors 24, 65 and -, by eight -, 49 and 88, 128 by eight 31, 60 and 84; with masks 128 by four 41, 89 and
-// 136, by eight -, 132 and 148; with alternatives, whose search is a CTA's, 128 by four 63, 83 and 111, 256 by two 112, 123 and 124,
-// but 1,000 rows of 100,000 fp32 97 and 108, 256 by four 86.
+// 136, by eight -, 132 and 148.  With 5 alternatives, whose search is a CTA's, 64 by four 39, 66 and 106, 128 by four 68, 82 and 107,
+// 256 by four 141, 137 and 124, but 1,500 masked rows of 50,001 fp32 128 by eight 71, 256 by four 69.  20 alternatives are the most that 64
+// threads take: with 32 more logits reach their bound than there are threads (1,200 and 8,000: 191 and 317, 128 by four 78 and 109).
+// With masks nine CTAs of 128 by four bf16 spare registers (8,192 of 32,000 167 -> 159 with one alternative).
 template <typename T, bool MASK, bool TOP>
 void launch_long(const RowArgs& a, const RowOut& o, cudaStream_t st) {
   const int vecs = a.vocab / Vec<T>::N;
@@ -979,8 +1010,9 @@ void launch_long(const RowArgs& a, const RowOut& o, cudaStream_t st) {
   while (log_parts < 3 && a.rows << (log_parts + 1) <= 2 * kNumSMs && a.vocab >> (log_parts + 1) >= 4096) ++log_parts;
   if (log_parts == 3) launch_cta<T, 256, 4, 4, MASK, TOP>(a, o, 3, st);
   else if (a.rows << log_parts <= 2 * kNumSMs) launch_cta<T, 512, 4, 2, MASK, TOP>(a, o, log_parts, st);
+  else if (TOP && vecs < 2048 && o.top <= 20) launch_cta<T, 64, 4, 20, MASK, TOP>(a, o, 0, st);
   else if (TOP && vecs >= 6000) launch_cta<T, 256, 4, 4, MASK, TOP>(a, o, 0, st);
-  else if (TOP || (MASK && vecs >= 512 && vecs < 6000)) launch_cta<T, 128, 4, 10, MASK, TOP>(a, o, 0, st);
+  else if (TOP || (MASK && vecs >= 512 && vecs < 6000)) launch_cta<T, 128, 4, TOP && MASK && Vec<T>::N == 8 ? 9 : 10, MASK, TOP>(a, o, 0, st);
   else if (vecs >= 3000) launch_cta<T, 128, 8, 7, MASK, false>(a, o, 0, st);
   else if (vecs >= 512) launch_cta<T, 64, 8, 14, MASK, false>(a, o, 0, st);
   else launch_cta<T, 64, 4, 20, MASK, false>(a, o, 0, st);

@@ -322,6 +322,25 @@ def test_alternatives_of_every_kind_of_row(dtype, rows, vocab, top):
         check_scores(xrl.xrl_logprob(part, top=top), part, None, None, 1.0, top)
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("vocab", [1031, 4100, 8190, 17000, 60000])
+@pytest.mark.parametrize("top", [3, 20, 21, 32])
+def test_alternatives_of_many_rows(dtype, vocab, top):
+    """Rows enough for a CTA each: random ones, with and without a mask, the best in one stretch, in one column of threads,
+    behind masked larger ones."""
+    rows, g = 600, torch.Generator(device="cuda").manual_seed(top)
+    x = torch.randn(rows, vocab, device="cuda", generator=g) * 3
+    at = torch.arange(vocab, device="cuda")
+    x[::5] += 20.0 * (at // 800 == 1)
+    x[1::5] += 20.0 * (at % 512 == 17)
+    x[2::5] = at * 1e-3
+    x[3::5] = -at * 1e-3
+    x = x.to(DTYPES[dtype])
+    mask = torch.rand(rows, vocab, device="cuda", generator=g) < 0.3
+    for m in (None, mask, (x < 2.0) & (at % 3 > 0)):
+        check_scores(xrl.xrl_logprob(x, mask=m, top=top), x, None, m, 1.0, top)
+
+
 def test_offsets_past_32_bits():
     """Rows 2^29 entries apart: the last ones start past 2^31 entries and 2^32 bytes."""
     stride, vocab, rows = 2 ** 29 + 8, 5000, 6
