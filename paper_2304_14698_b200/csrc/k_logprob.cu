@@ -209,11 +209,17 @@ __global__ void __launch_bounds__(128) k_logprob_warp(RowArgs a, RowOut o) {
     Given given;
     if (lane == 0) given = given_of<T>(a, row);
     float v[E];
+    uint8_t left[MASK ? E : 1];
+    const uint8_t* mask = MASK ? a.mask + row * a.mask_stride : nullptr;
 #pragma unroll
     for (int e = 0; e < E; ++e) {
       const int j = e * 32 + lane;
       v[e] = j < a.vocab ? load1(x + j) : kNegInf;
-      if (MASK && j < a.vocab && !__ldg(a.mask + row * a.mask_stride + j)) v[e] = kNegInf;
+      if (MASK) left[e] = j < a.vocab ? __ldg(mask + j) : uint8_t(0);
+    }
+    if (MASK) {                          // (after all loads)
+#pragma unroll
+      for (int e = 0; e < E; ++e) v[e] = left[e] ? v[e] : kNegInf;
     }
     float m = kNegInf;
 #pragma unroll
@@ -236,10 +242,24 @@ __global__ void __launch_bounds__(128) k_logprob_warp(RowArgs a, RowOut o) {
     const bool empty = q.s == 0.f;
     const RowNorm n = {m, empty ? kNegInf : kLn2 * log2f(q.s)};
     if (lane == 0) write_row(a, o, row, given, n, empty ? 0.f : entropy_of(q));
-    if (o.top) {
-      Best mine, last;
+    if (o.top) {                         // the best of the lanes' best is taken out, `top` times; of equals the lowest index
+      Best mine;
+      for (int k = 0; k < o.top; ++k) {
+        float best = kNegInf;
+        int at = 0;
 #pragma unroll
-      for (int e = 0; e < E; ++e) offer(mine, last, v[e], e * 32 + lane, o.top, lane);
+        for (int e = 0; e < E; ++e)
+          if (v[e] > best) { best = v[e]; at = e; }
+        const uint32_t key = key_of(best), most = __reduce_max_sync(kAll, key);
+        if (most == key_of(kNegInf)) break;
+        const unsigned i = __reduce_min_sync(kAll, key == most ? unsigned(at * 32 + lane) : kAll);
+        const float taken = __shfl_sync(kAll, best, i & 31);
+        if (lane == k) { mine.v = taken; mine.i = int32_t(i); }
+        if (lane == int(i & 31))
+#pragma unroll
+          for (int e = 0; e < E; ++e)
+            if (e == at) v[e] = kNegInf;
+      }
       write_top(a, o, row, n, mine, lane);
     }
   }
@@ -1021,6 +1041,13 @@ template <typename T, bool MASK>
 bool launch_rows(const RowArgs& a, const RowOut& o, cudaStream_t st) {
   if (a.vocab > 1024) {
     o.top ? launch_long<T, MASK, true>(a, o, st) : launch_long<T, MASK, false>(a, o, st);
+    return true;
+  }
+  // What a warp takes out of registers one by one soon costs more than a CTA's search (us, 16 and 16,384 rows of 1,000 fp32, 5
+  // alternatives 4.1 and 29, by CTAs 4.1 and 35; 20: 8.6 and 81, 5.8 and 45)
+  if (o.top > 8 && a.vocab > 512) {
+    if (o.top <= 20) launch_cta<T, 64, 4, 20, MASK, true>(a, o, 0, st);
+    else launch_cta<T, 128, 4, MASK && Vec<T>::N == 8 ? 9 : 10, MASK, true>(a, o, 0, st);
     return true;
   }
   const int64_t ctas = (a.rows + 3) / 4;

@@ -323,10 +323,10 @@ def test_alternatives_of_every_kind_of_row(dtype, rows, vocab, top):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
-@pytest.mark.parametrize("vocab", [1031, 4100, 8190, 17000, 60000])
+@pytest.mark.parametrize("vocab", [61, 129, 500, 801, 1031, 4100, 8190, 17000, 60000])
 @pytest.mark.parametrize("top", [3, 20, 21, 32])
 def test_alternatives_of_many_rows(dtype, vocab, top):
-    """Rows enough for a CTA each: random ones, with and without a mask, the best in one stretch, in one column of threads,
+    """Rows enough for a warp or a CTA each: random ones, with and without a mask, the best in one stretch, in one column of threads,
     behind masked larger ones."""
     rows, g = 600, torch.Generator(device="cuda").manual_seed(top)
     x = torch.randn(rows, vocab, device="cuda", generator=g) * 3
