@@ -363,8 +363,10 @@ xrl_status xrl_logprob_grad(int32_t device, int32_t dtype, int32_t rows, int32_t
  * (X^T X and products from the right for matrices with more rows than columns: the same in exact arithmetic).  Momentum,
  * learning rate and the choice of matrices are the caller's.
  *   dtype      XRL_FP32 or XRL_BF16, of G and of the result.  The products run on the tensor cores with fp32 accumulators:
- *              for bf16 from operands of 11 bits with the diagonals of A and its polynomial kept in fp32 (an error of some
- *              1e-3 of the result's norm before its rounding to bf16, which is 1.7e-3); for fp32 from operands of 22 bits
+ *              for bf16 from operands of 11 bits with the diagonals of A and its polynomial kept in fp32 (an error of 1e-4 to
+ *              1.3e-3 of the result's norm, before its rounding to bf16 of 1.7e-3, where the operands' roundings average out; where
+ *              they all go one way, as in matrices of rank one whose entries have one size, up to 1.4e-2: singular values are off
+ *              by that, the directions are not); for fp32 from operands of 22 bits (some 1e-6; up to 5e-5 for matrices of low rank)
  *   batch      matrices, batch_stride elements apart, rows row_stride apart (row_stride >= cols; the matrices must not
  *              overlap); each side at most XRL_MAX_SIDE
  *   steps      1 to 64 (5 is usual);   eps > 0 (1e-7 is usual): G = 0 gives 0, and so may a G whose norm is far below eps

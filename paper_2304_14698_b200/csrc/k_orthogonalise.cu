@@ -7,8 +7,10 @@
 // the diagonals of A and B, whose entries outweigh all others: D_A and D_B are held apart in fp32, and with A = D_A + F
 //   B_ij = b F_ij + c ((d_i + d_j) F_ij + (F F)_ij),   X' = (a + D_B) X + (B - D_B) X
 // only the small rest goes through the tensor cores.  (2-norm error of five steps before the result's rounding, matrices of
-// 64 to 4,096: 1e-4 to 1.3e-3, 2 to 7 times less than with the diagonals inside; rounding to bf16 is 1.7e-3.)  bf16 updates
-// take one product of hi parts; fp32 ones add hi lo and lo hi, which leaves 2^-22 of an entry.
+// 64 to 4,096 with random entries: 1e-4 to 1.3e-3, 2 to 7 times less than with the diagonals inside; rounding to bf16 is 1.7e-3.
+// Where entries have one size their roundings do not average out, and X's, F's and B's go into every product the same way: all
+// ones, or signs of rank one, 1e-3 to 1.4e-2, 256 square 1.28e-2.)  bf16 updates take one product of hi parts; fp32 ones add
+// hi lo and lo hi, which leaves 2^-22 of an entry.
 // A and B are symmetric: only tiles on and above the diagonal are computed, and stored twice.
 //
 // Bound by the tensor cores for large matrices; by the chain of 3 * steps launches for small ones.
