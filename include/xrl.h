@@ -375,7 +375,8 @@ xrl_status xrl_logprob_grad(int32_t device, int32_t dtype, int32_t rows, int32_t
  *   workspace  DEVICE, 256-byte aligned, of at least the bytes that xrl_orthogonalise_workspace says (HOST output; about 8 bytes
  *              per entry of G and of the smaller Gram matrix).  It holds nothing between calls; calls that may run at the
  *              same time need one each
- *   device_status  DEVICE int32 [1] or NULL: XRL_OK, or XRL_ERR_TIMEOUT if a bounded wait ran out (the results are undefined then)
+ *   device_status  DEVICE int32 [1] or NULL: XRL_OK, or XRL_ERR_TIMEOUT if a bounded wait ran out, or XRL_ERR_UNSUPPORTED if shared
+ *              memory did not start where the tiles need it.  With or without it, what could not be computed is NaN in the result
  * A matrix with a NaN or an infinity becomes NaN; the others of its batch are not affected.  A call's results are the same
  * bits every time; a matrix's last bits may depend on how many share its call (the tiles are chosen by that).  Needs no context; 2 + 3 * steps launches at most; captures into a CUDA graph.
  * Errors: INVALID_ARG, UNSUPPORTED (sizes), CUDA. */

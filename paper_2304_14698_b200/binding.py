@@ -510,7 +510,7 @@ def xrl_orthogonalise(grad, steps=5, eps=1e-7, out=None, workspace=None, device_
     """Orthogonalised updates by Newton-Schulz products (see include/xrl.h).  grad: torch CUDA [rows, cols] or [batch, rows,
     cols], float32 or bfloat16, entries of a row side by side; out: the same shape and type, may be grad itself, allocated
     (contiguous) if None; workspace: uint8 tensor of xrl_orthogonalise_workspace bytes, allocated if None (on the call's
-    stream, so it is safe to let go); device_status: int32 [1] or None."""
+    stream, so it is safe to let go); device_status: int32 [1] or None; what a wait that ran out left uncomputed is NaN."""
     where = "xrl_orthogonalise"
     torch = _th()
     if stream is not None and (out is None or workspace is None) and grad.is_cuda:
@@ -547,14 +547,14 @@ def layer_matrices(m, blob):
     return blob.as_strided((L, H, H), (apart, H, 1), blob.storage_offset() + first)
 
 
-def orthogonalise_layers(m, grad, steps=5, eps=1e-7, stream=None):
+def orthogonalise_layers(m, grad, steps=5, eps=1e-7, stream=None, device_status=None):
     """In place: the layer matrices' part of an xrl_ppo_grad gradient becomes the orthogonalised update; the rest of the blob
-    stays the gradient."""
+    stays the gradient.  device_status as for xrl_orthogonalise."""
     if grad.dim() != 1 or not grad.is_contiguous():
         raise XrlError(1, "orthogonalise_layers (grad: a contiguous blob)")
     if m["L"] > 0:
         w = layer_matrices(m, grad)
-        xrl_orthogonalise(w, steps, eps, out=w, stream=stream)
+        xrl_orthogonalise(w, steps, eps, out=w, device_status=device_status, stream=stream)
     return grad
 
 

@@ -15,7 +15,8 @@
 //
 // Bound by the tensor cores for large matrices; by the chain of 3 * steps launches for small ones.
 // Every wait on an mbarrier is bounded; on expiry the kernel records XRL_ERR_TIMEOUT, lets its copies in flight land, frees
-// its tensor memory and returns.
+// its tensor memory and returns.  The last product then writes NaN: all over when it finds the word set by a launch before
+// it, else what a warp had to write whose wait ran out.  No caller takes such a result for an update.
 #include <cuda_fp16.h>
 
 #include <cmath>
@@ -498,6 +499,12 @@ __device__ __forceinline__ bool finish(const Maps& maps, const NsArgs& a, Pieces
   return true;
 }
 
+// NaN for the caller in place of a piece of up to 32 rows and `cols` columns
+template <typename T> __device__ __noinline__ void write_none(T* out, int64_t ld, int rows, int cols) {
+  for (int y = 0; y < rows && y < 32; ++y)
+    for (int x = threadIdx.x & 31; x < cols; x += 32) out[y * ld + x] = T(NAN);
+}
+
 __device__ __forceinline__ void prefetch_map(const CUtensorMap* m) {
   asm volatile("prefetch.tensormap [%0];" ::"l"(m) : "memory");
 }
@@ -549,11 +556,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_ns_product(const __grid_constan
   tile_sync<CTAS>();
   tc_fence_after();
   const uint32_t tmem_base = __shfl_sync(0xFFFFFFFFu, *tmem_slot, 0);
-  int total = a.total;
-  if ((base & 1023u) != 0) {             // the swizzle's pattern starts on 1,024 bytes
-    total = 0;
-    if (threadIdx.x == 0) raise(a.status, XRL_ERR_UNSUPPORTED);
-  }
+  const int total = a.total;
+  const bool sound = (base & 1023u) == 0;                // the swizzle's pattern starts on 1,024 bytes
+  auto give_up = [&]() { raise(a.status, sound ? XRL_ERR_TIMEOUT : XRL_ERR_UNSUPPORTED); };
   const int all_ksteps = (a.k + kStep - 1) / kStep;
   const int kbegin = SPLIT ? all_ksteps * part / group : 0;
   const int ksteps = SPLIT ? all_ksteps * (part + 1) / group - kbegin : all_ksteps;
@@ -566,7 +571,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_ns_product(const __grid_constan
   // that lane some 115 cycles, and a 256 x 256 x 16 product takes 128: 4,096 square bf16 1,504 us.)
   if (warp == 0) {
     uint32_t it = 0;
-    bool ok = true;
+    bool ok = sound;
     fence_async_all();
     for (int tile = first; ok && tile < total; tile += step) {
       const Tile t = tile_of<C::M, C::N, SYM>(a, tile);
@@ -589,7 +594,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_ns_product(const __grid_constan
       }
     }
     if (!ok) {
-      if (lane == 0) raise(a.status, XRL_ERR_TIMEOUT);
+      if (lane == 0) give_up();
       let_copies_land();
     }
   } else if (warp == 1) {
@@ -602,7 +607,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_ns_product(const __grid_constan
       const uint64_t a0 = operand_desc<A_MN>(base, 0), b0 = operand_desc<B_MN>(base + C::OFF_B, 0);
       constexpr int A_K = (A_MN ? 2048 : 32) >> 4, B_K = (B_MN ? 2048 : 32) >> 4, A_LO = C::A_BYTES >> 4, B_LO = C::B_BYTES >> 4;
       uint32_t it = 0, lt = 0;
-      bool ok = true;
+      bool ok = sound;
       for (int tile = first; ok && tile < total; tile += step) {
         for (int k0 = 0; ok && k0 < ksteps; k0 = k0 < ksteps - C::CHUNK ? k0 + C::CHUNK : ksteps, ++lt) {
           const int k1 = k0 < ksteps - C::CHUNK ? k0 + C::CHUNK : ksteps, buf = lt & 1;
@@ -640,7 +645,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_ns_product(const __grid_constan
           }
         }
       }
-      if (!ok && lane == 0) raise(a.status, XRL_ERR_TIMEOUT);
+      if (!ok && lane == 0) give_up();
     }
   } else if (warp - 2 < C::WORKERS) {
     constexpr int WC = C::WARP_COLS;
@@ -651,7 +656,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_ns_product(const __grid_constan
     w.bar = bar_in(warp - 2);
     w.lane = lane;
     uint32_t lt = 0;
-    bool ok = true;
+    bool ok = sound;
+    const bool broken = MODE == APPLY && a.user && *static_cast<volatile int32_t*>(a.status) != XRL_OK;      // an earlier launch
     for (int tile = first; ok && tile < total; tile += step) {
       const Tile t = tile_of<C::M, C::N, SYM>(a, tile);
       const int row = t.row + rank * kRows + q * 32, col = t.col + side * WC;
@@ -723,8 +729,17 @@ __global__ void __launch_bounds__(kThreads, 1) k_ns_product(const __grid_constan
       }
     }
     if (!ok) {
-      if (lane == 0) raise(a.status, XRL_ERR_TIMEOUT);
+      if (lane == 0) give_up();
       let_copies_land();
+    }
+    if (MODE == APPLY && a.user && (broken || !ok)) {    // (what it has written of the result too)
+      typedef typename std::conditional<NPROD == 1, bf16, float>::type T;
+      __syncwarp();
+      for (int tile = first; tile < total; tile += step) {
+        const Tile t = tile_of<C::M, C::N, SYM>(a, tile);
+        const int row = t.row + rank * kRows + q * 32, col = t.col + side * WC;
+        write_none(static_cast<T*>(a.user) + t.z * a.user_batch + row * a.user_ld + col, a.user_ld, a.m - row, min(a.n - col, WC));
+      }
     }
     if (lane == 0) tma_wait_read<0>();   // (the launch ends when what they write is there)
   }
