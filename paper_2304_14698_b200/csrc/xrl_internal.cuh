@@ -113,9 +113,11 @@ inline bool ensure_dynamic_smem(Kernel kernel, int bytes, bool (&done)[64]) {
 // kernel that has entered has its predecessor complete, and that one its own, so every earlier kernel of the stream is.
 // What it saves is the gap between kernels: training step of 36 k fp32 rows (40 kernels) 579 -> 514 us, 3.5 k rows of
 // hidden 64 in 50 kernels 346 -> 273, delta step 508 -> 463, 124 k rows of hidden 192 (16 kernels) 334 -> 303.
-// No kernel lets its dependents start earlier (griddepcontrol.launch_dependents): their waiting CTAs take places beside
-// the running kernel's, several on one SM while others stay empty (the same four: 536, 309, 498, 304 with the signal
+// No kernel of a step lets its dependents start earlier (griddepcontrol.launch_dependents): their waiting CTAs take places
+// beside the running kernel's, several on one SM while others stay empty (the same four: 536, 309, 498, 304 with the signal
 // first, 531, 305, 495, 304 behind enter(); a training step whose last product has 60 CTAs became slower than without).
+// The small products inside one orthogonalised update do, behind their own enter(): their dependents are the next product's
+// CTAs, which take an SM each.  Its last product does not, so whatever is launched behind an update starts as behind any other.
 __device__ __forceinline__ void enter() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 template <typename... P, typename... A>
 inline void launch(void (*kernel)(P...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, A&&... args) {
