@@ -335,9 +335,11 @@ xrl_status xrl_gae(int32_t device, int32_t num_steps, int32_t num_trajectories, 
  *   top_token   DEVICE int32 [rows x num_top], top_logp DEVICE fp32 [rows x num_top]: the num_top (0 to XRL_MAX_TOP, at most
  *               vocab) largest logits of the support in falling order, equal ones by rising index, and their ln p; -1 and
  *               -infinity where the support has fewer
- * A row with a NaN or +infinity in its support gives NaN in logp, entropy, l and top_logp; its alternatives are the best of
- * its other entries.  The order of a row's sum depends on the sizes and on how far the row's first entry is from a 16-byte
- * boundary alone.  Needs no context; one launch; captures into a CUDA graph; nothing is allocated.  Errors: INVALID_ARG, UNSUPPORTED (num_top), CUDA. */
+ * A row with a NaN or +infinity in its support gives NaN in logp (a token outside the support still -infinity), entropy, l and
+ * top_logp; NaN entries are no alternatives, +infinity comes before all others.  The order of a row's sum depends on the sizes, on
+ * how far the row's first entry is from a 16-byte boundary, on whether there is a mask, and on num_top: the same call gives the
+ * same bits, calls that differ in these the same up to rounding.  Needs no context; one launch; captures into a CUDA graph; nothing
+ * is allocated.  Errors: INVALID_ARG, UNSUPPORTED (num_top), CUDA. */
 #define XRL_MAX_TOP 32
 xrl_status xrl_logprob(int32_t device, int32_t dtype, int32_t rows, int32_t vocab, const void* logits, int64_t row_stride,
                        const int32_t* token, const uint8_t* mask, int64_t mask_stride, float scale, int32_t num_top,

@@ -81,6 +81,35 @@ def test_edges_of_the_range_in_many_rows(dtype, vecs, masked):
             assert bool((o["top_token"][5::n, 0] == 1).all()) and not bool((o["top_token"][::n] == vocab - 1).any())
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows,vocab", [(4, 50), (4, 1000), (4, 1500), (4, 90000), (ROWS, 1500), (ROWS, 30001)])
+@pytest.mark.parametrize("top", [0, 3, 32])
+def test_rows_with_numbers_that_are_none(dtype, rows, vocab, top):
+    """NaN or +infinity in the support: NaN for a choice inside the support, -infinity for one outside it; NaN entries are no
+    alternatives, infinite ones come first, the lower index before the higher."""
+    x, token, mask, _ = make(dtype, rows, vocab, rows + vocab)
+    x, mask[:] = x.clone(), 1
+    broken = x[::2]
+    x[::2, 7] = math.nan
+    x[1::2, 9], x[1::2, 30] = INF, INF
+    x[:, 11] = -INF
+    mask[:, 13] = 0
+    for t in (7, 9, 11, 13, 20):
+        token[:] = t
+        o = xrl.xrl_logprob(x, token, mask=mask, top=top)
+        if t in (11, 13):
+            assert bool((o["logp"] == -INF).all())
+        else:
+            assert bool(torch.isnan(o["logp"]).all())
+        assert bool(torch.isnan(o["entropy"]).all()) and bool(torch.isnan(o["norm"][:, 1]).all())
+    if top:
+        assert bool((o["top_token"][1::2, 0] == 9).all()) and bool((o["top_token"][1::2, 1] == 30).all())
+        z = broken.float().masked_fill(mask[::2] == 0, -INF).masked_fill(torch.isnan(broken), -INF)
+        v, i = torch.sort(z, dim=1, descending=True, stable=True)
+        assert torch.equal(o["top_token"][::2], i.masked_fill(v == -INF, -1)[:, :top].int())
+        assert torch.equal(torch.isnan(o["top_logp"]), o["top_token"] >= 0)
+
+
 # (rows, vocab): pieces of 1,024 vectors for each of the 592 CTAs that stay, several times over; vocabularies of a few entries more
 # than whole pieces, whose last piece is empty in the rows that start with single entries
 PIECES = [(700, 4099), (700, 8195), (1300, 2049), (300, 33001), (650, 16389)]
