@@ -378,6 +378,9 @@ def _stream_scope(stream, device):
     return th.cuda.stream(s)
 
 
+_MOST = 2 ** 31 - 1                        # of the C ABI's int32 sizes: ctypes would pass the lowest 32 bits of more
+
+
 def _flat(where, what, t, dtype, shape):
     """The pointer of an argument that has to be a contiguous tensor of this type and shape (or None)."""
     if t is None:
@@ -425,6 +428,8 @@ def xrl_logprob(logits, token=None, mask=None, scale=1.0, top=0, out=None, strea
     if len(shape) != 2:
         raise XrlError(1, f"{where} (logits: [rows x vocab])")
     rows, vocab = shape
+    if rows > _MOST or vocab > _MOST or top > _MOST:
+        raise XrlError(8, f"{where} (sizes up to 2^31 - 1)")
     f32 = th.float32
     dev = _device_of(where, logits, token, mask)
     dtype = _storage(where, logits)
@@ -473,6 +478,8 @@ def xrl_logprob_grad(logits, norm, token=None, dlogp=None, entropy=None, dentrop
     if len(shape) != 2:
         raise XrlError(1, f"{where} (logits: [rows x vocab])")
     rows, vocab = shape
+    if rows > _MOST or vocab > _MOST:
+        raise XrlError(8, f"{where} (sizes up to 2^31 - 1)")
     f32, each = th.float32, (rows,)
     dev = _device_of(where, logits, norm, token, dlogp, entropy, dentropy, mask, grad)
     dtype = _storage(where, logits)
@@ -494,6 +501,8 @@ def xrl_logprob_grad(logits, norm, token=None, dlogp=None, entropy=None, dentrop
 
 
 def xrl_orthogonalise_workspace(dtype, batch, rows, cols) -> int:
+    if max(batch, rows, cols) > _MOST:
+        raise XrlError(8, "xrl_orthogonalise_workspace (sizes up to 2^31 - 1)")
     n = C.c_size_t()
     _check(load_library().xrl_orthogonalise_workspace(dtype, batch, rows, cols, C.byref(n)), "xrl_orthogonalise_workspace")
     return int(n.value)
@@ -520,6 +529,10 @@ def xrl_orthogonalise(grad, steps=5, eps=1e-7, out=None, workspace=None, device_
         raise XrlError(1, f"{where} (grad: [rows x cols] or [batch x rows x cols])")
     rows, cols = grad.shape[-2:]
     batch = grad.shape[0] if grad.dim() == 3 else 1
+    if max(batch, rows, cols) > _MOST:
+        raise XrlError(8, f"{where} (sizes up to 2^31 - 1)")
+    if not 1 <= steps <= 64:
+        raise XrlError(1, f"{where} (steps: 1 to 64)")
     dev = _device_of(where, grad, out, workspace, device_status)
     dtype = _storage(where, grad)
     if out is None:
