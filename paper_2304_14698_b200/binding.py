@@ -557,6 +557,8 @@ def layer_matrices(m, blob):
     model_config)."""
     H, L = m["H"], m["L"]
     first, apart = (2 * m["S"] + m["T"]) * H + H, H * H + 3 * H
+    if blob.dim() != 1 or not blob.is_contiguous() or blob.numel() < first + L * apart:
+        raise XrlError(1, "layer_matrices (blob: contiguous, of the model's size)")
     return blob.as_strided((L, H, H), (apart, H, 1), blob.storage_offset() + first)
 
 

@@ -29,6 +29,20 @@ def test_refused(call):
     assert e.value.status == 8
 
 
+def test_layers_of_a_blob_that_is_none():
+    """A view that skips entries, one whose storage goes on behind it, and a table."""
+    m = dict(T=13, S=8, H=64, K=2, L=3, Hm=32, Dg=1, dtype="fp32", A_max=8)
+    size = (2 * 8 + 13) * 64 + 64 + 3 * (64 * 64 + 3 * 64)
+    assert xrl.layer_matrices(m, torch.zeros(size)).shape == (3, 64, 64)
+    for bad in (torch.zeros(2 * size)[::2], torch.zeros(2 * size)[:size - 1], torch.zeros(1, size), torch.zeros(size - 1)):
+        with pytest.raises(xrl.XrlError) as e:
+            xrl.layer_matrices(m, bad)
+        assert e.value.status == 1
+    for bad in (torch.zeros(2 * size)[::2], torch.zeros(2 * size)[:size - 1]):
+        with pytest.raises(xrl.XrlError):
+            xrl.orthogonalise_layers(m, bad)
+
+
 @pytest.mark.parametrize("steps", [0, -1, 65, MANY, 5 - 2 ** 32])
 def test_steps(steps):
     with pytest.raises(xrl.XrlError) as e:
