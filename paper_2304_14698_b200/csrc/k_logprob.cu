@@ -539,7 +539,7 @@ template <int THREADS> __device__ __forceinline__ void rank_candidates(Candidate
 template <typename T, int THREADS, bool MASK>
 __device__ __forceinline__ void best_of_part(const Row<T>& r, int v0, int v1, bool edges, float thread_max, float part_max, int stretches, int stretch, int k,
                                              Candidates<THREADS>& s, uint32_t* red) {
-  constexpr int N = Vec<T>::N, U = 4, W = THREADS / 32, GROUP = THREADS / 32;
+  constexpr int N = Vec<T>::N, U = 4, GROUP = THREADS / 32;
   static_assert(GROUP <= 32, "32 groups of threads");
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const uint32_t mine = key_of(thread_max);
@@ -631,7 +631,7 @@ __device__ __forceinline__ void best_of_part(const Row<T>& r, int v0, int v1, bo
 template <typename T, int THREADS, int U, int CTAS, bool MASK, bool TOP>
 __global__ void __launch_bounds__(THREADS, CTAS) k_logprob_cta(RowArgs a, RowOut o, int log_parts) {
   enter();
-  constexpr int N = Vec<T>::N, W = THREADS / 32, GROUP = U * THREADS;
+  constexpr int W = THREADS / 32, GROUP = U * THREADS;
   __shared__ Sums s_sums[W];
   __shared__ float s_red[64];
   __shared__ __align__(16) Candidates<TOP ? THREADS : 32> s_best;
@@ -1017,25 +1017,42 @@ void launch_cta(const RowArgs& a, const RowOut& o, int log_parts, cudaStream_t s
   launch_cluster(k_logprob_cta<T, THREADS, U, CTAS, MASK, TOP>, unsigned(a.rows << log_parts), THREADS, 0, 1 << log_parts, st, a, o,
                  log_parts);
 }
-// Threads, vectors a thread has in flight, CTAs an SM holds.  Measured in us, 16,384 rows of 1,200 and 8,000, 8,192 of 32,000, bf16:
-// 64 threads by four vectors 24, 65 and -, by eight -, 49 and 88, 128 by eight 31, 60 and 84; with masks 128 by four 41, 89 and
-// 136, by eight -, 132 and 148.  With 5 alternatives, whose search is a CTA's, 64 by four 39, 66 and 106, 128 by four 68, 82 and 107,
-// 256 by four 141, 137 and 124, but 1,500 masked rows of 50,001 fp32 128 by eight 71, 256 by four 69.  20 alternatives are the most that 64
-// threads take: with 32 more logits reach their bound than there are threads (1,200 and 8,000: 191 and 317, 128 by four 78 and 109).
-// With masks nine CTAs of 128 by four bf16 spare registers (8,192 of 32,000 167 -> 159 with one alternative).
+// Threads, vectors a thread has in flight, CTAs an SM holds; rows of so many 16-byte vectors.  Measured in us, 200 MB of logits where
+// no rows are given (bf16 / fp32):
+// - without alternatives: 64 by four 61 / 53 at 300 vectors, 48 / 43 at 600, 47 / 42 at 4,000; 64 by eight 72 / 59, 51 / 47 and 42 / 37,
+//   at 1,500 38 / 34; 128 by eight 38 / 35 at 4,000, 37 / 34 at 3,000, at 1,500 51 / 48.  With masks 64 by four 67 / 54 at 600,
+//   60 / 48 at 1,500, 73 / 60 at 4,000; 128 by four 72 / 62, 61 / 53 and 63 / 53; 128 by eight 66 / 57 at 4,000, at 6,500 60 / 45
+//   where 128 by four takes 64 / 53.
+// - with 20 alternatives, whose search is a CTA's: 64 by four 89 / 79 at 600, 57 / 52 at 1,500, 59 / 55 at 2,200; 128 by four 105 / 94,
+//   61 / 54 and 56 / 53; 256 by four 188 / 168, 101 / 89 and 78 / 69.  20 are the most that 64 threads take: with 32 more logits reach
+//   their bound than there are threads (600: 330 / 215, 128 by four 123 / 108).
+// - 256 threads for long rows: with masks and 5 alternatives at 9,000 vectors 99 / 80 for 2,200 rows, 133 / 111 for 3,000, 128 by four
+//   101 / 86 and 132 / 118; at 12,500 94 / 74 for 1,500 rows and 171 / 138 for 3,000, 128 by four 105 / 98 and 177 / 160.  Without masks
+//   they lose up to 12,000 vectors (6,500: fp32 1,000 rows 24 -> 28, 3,000 64 -> 73; 9,000: bf16 5,000 rows 131 -> 147) but
+//   where rows are few (fp32 400 rows of 9,000 24 -> 17, of 6,500 18 -> 15); behind that they lose 2 to 9 % with 5 alternatives and win as
+//   much with 20 (fp32 12,500, 2,200 rows: 82 -> 84, 94 -> 89).
+// - masked searches in bf16 keep their registers by nine CTAs of 128 in place of ten: 5 alternatives at 3,000 74 -> 71, at 4,000
+//   78 -> 71, at 6,500 77 -> 68; below 1,000 vectors the tenth is worth more (32 alternatives at 160 475 -> 413, at 600 172 -> 160).
 template <typename T, bool MASK, bool TOP>
 void launch_long(const RowArgs& a, const RowOut& o, cudaStream_t st) {
   const int vecs = a.vocab / Vec<T>::N;
   int log_parts = 0;                     // few rows: clusters, no CTA with less than 4,096 entries
   while (log_parts < 3 && a.rows << (log_parts + 1) <= 2 * kNumSMs && a.vocab >> (log_parts + 1) >= 4096) ++log_parts;
-  if (log_parts == 3) launch_cta<T, 256, 4, 4, MASK, TOP>(a, o, 3, st);
-  else if (a.rows << log_parts <= 2 * kNumSMs) launch_cta<T, 512, 4, 2, MASK, TOP>(a, o, log_parts, st);
-  else if (TOP && vecs < 2048 && o.top <= 20) launch_cta<T, 64, 4, 20, MASK, TOP>(a, o, 0, st);
-  else if (TOP && vecs >= 6000) launch_cta<T, 256, 4, 4, MASK, TOP>(a, o, 0, st);
-  else if (TOP || (MASK && vecs >= 512 && vecs < 6000)) launch_cta<T, 128, 4, TOP && MASK && Vec<T>::N == 8 ? 9 : 10, MASK, TOP>(a, o, 0, st);
-  else if (vecs >= 3000) launch_cta<T, 128, 8, 7, MASK, false>(a, o, 0, st);
-  else if (vecs >= 512) launch_cta<T, 64, 8, 14, MASK, false>(a, o, 0, st);
-  else launch_cta<T, 64, 4, 20, MASK, false>(a, o, 0, st);
+  if (log_parts == 3) return launch_cta<T, 256, 4, 4, MASK, TOP>(a, o, 3, st);
+  if (a.rows << log_parts <= 2 * kNumSMs) return launch_cta<T, 512, 4, 2, MASK, TOP>(a, o, log_parts, st);
+  if constexpr (TOP) {
+    if (vecs < 2048 && o.top <= 20) return launch_cta<T, 64, 4, 20, MASK, TOP>(a, o, 0, st);
+    if (vecs >= 6000 && (MASK || vecs >= 12000 || a.rows <= 4 * kNumSMs)) return launch_cta<T, 256, 4, 4, MASK, TOP>(a, o, 0, st);
+    if constexpr (MASK && Vec<T>::N == 8) {
+      if (vecs >= 1000) return launch_cta<T, 128, 4, 9, MASK, TOP>(a, o, 0, st);
+    }
+    launch_cta<T, 128, 4, 10, MASK, TOP>(a, o, 0, st);
+  } else {
+    if (vecs < (MASK ? 2000 : 512)) return launch_cta<T, 64, 4, 20, MASK, TOP>(a, o, 0, st);
+    if (vecs >= (MASK ? 6000 : 3000)) return launch_cta<T, 128, 8, 7, MASK, TOP>(a, o, 0, st);
+    if constexpr (MASK) launch_cta<T, 128, 4, 10, MASK, TOP>(a, o, 0, st);
+    else launch_cta<T, 64, 8, 14, MASK, TOP>(a, o, 0, st);
+  }
 }
 template <typename T, bool MASK>
 bool launch_rows(const RowArgs& a, const RowOut& o, cudaStream_t st) {
@@ -1047,7 +1064,7 @@ bool launch_rows(const RowArgs& a, const RowOut& o, cudaStream_t st) {
   // alternatives 4.1 and 29, by CTAs 4.1 and 35; 20: 8.6 and 81, 5.8 and 45)
   if (o.top > 8 && a.vocab > 512) {
     if (o.top <= 20) launch_cta<T, 64, 4, 20, MASK, true>(a, o, 0, st);
-    else launch_cta<T, 128, 4, MASK && Vec<T>::N == 8 ? 9 : 10, MASK, true>(a, o, 0, st);
+    else launch_cta<T, 128, 4, 10, MASK, true>(a, o, 0, st);
     return true;
   }
   const int64_t ctas = (a.rows + 3) / 4;

@@ -13,9 +13,9 @@ pytestmark = pytest.mark.gpu
 ROWS = 320                                 # more than clusters, or a CTA on every SM twice, are used for
 WIDTH = {"fp32": 4, "bf16": 8}             # entries of a 16-byte vector
 
-# Vectors of a row: about 512, 3,000 and 6,000, where threads and vectors a thread has in flight change; with the rest
+# Vectors of a row: about 512, 2,000, 3,000 and 6,000, where threads and vectors a thread has in flight change; with the rest
 # behind whole groups (256 vectors up to there, 512 and 1,024 then) none, a few, just under half of one and just over
-VECS = [257, 383, 385, 511, 512, 525, 767, 769, 1023, 1024, 1290, 2999, 3000, 3583, 3585, 4096, 4100, 5999, 6000, 6144]
+VECS = [257, 383, 385, 511, 512, 525, 767, 769, 1023, 1024, 1290, 1999, 2000, 2302, 2306, 2999, 3000, 3583, 3585, 4096, 4100, 5999, 6000, 6144]
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
