@@ -863,8 +863,9 @@ bool launch_product(const Operand& left, const Operand& right, const Operand* in
     return (MODE == APPLY ? tm * tn : tm * (tm + 1) / 2 * (m / n)) * batch;
   };
   // (where a pair has less than two tiles of a short reduction to apply, smaller ones let one's epilogue run under the next one's
-  // products: 4,100 x 1,001 209 -> 203 us, 1,024 x 4,096 183 -> 179; but 2,048 square 238 -> 244, 2,800 450 -> 503)
-  const bool shallow = MODE == APPLY && NPROD == 1 && a.k <= 1024 && tiles(256, WIDE) < kNumSMs && tiles(128, 128) > kNumSMs;
+  // products: 5,000 x 800 225 -> 197 us, 800 x 5,000 220 -> 196, 600 x 8,000 250 -> 237, 4,100 x 1,001 207 -> 204, two of 2,048 x 1,024
+  // 187 -> 184; but 2,048 square 233 -> 241, 2,800 460 to 505 -> 570, and 1,280 x 5,120 would still gain, 264 -> 258)
+  const bool shallow = MODE == APPLY && NPROD == 1 && a.k <= 1024 && tiles(256, WIDE) < kNumSMs;
   const int kind = !shallow && tiles(256, WIDE) >= 60 && a.m > 128 && a.n > 128 ? 2
                    : NPROD == 1 && tiles(128, 128) >= 100 && a.n > 64 ? 1 : 0;
   // A long reduction of few tiles: one tile to a cluster, and shares that are worth the meeting, some 3 us: 12 stages of one
