@@ -369,8 +369,9 @@ xrl_status xrl_logprob_grad(int32_t device, int32_t dtype, int32_t rows, int32_t
  *              1.3e-3 of the result's norm, before its rounding to bf16 of 1.7e-3, where the operands' roundings average out; where
  *              they all go one way, as in matrices of rank one whose entries have one size, up to 1.4e-2: singular values are off
  *              by that, the directions are not); for fp32 from operands of 22 bits (some 1e-6; up to 5e-5 for matrices of low rank)
- *   batch      matrices, batch_stride elements apart, rows row_stride apart (row_stride >= cols; the matrices must not
- *              overlap); each side at most XRL_MAX_SIDE
+ *   batch      matrices, batch_stride elements apart, rows row_stride apart (row_stride >= cols, and each matrix ends
+ *              before the next begins: matrices side by side in the rows of a wider one take a call each); each side at most
+ *              XRL_MAX_SIDE
  *   steps      1 to 64 (5 is usual);   eps > 0 (1e-7 is usual): G = 0 gives 0, and so may a G whose norm is far below eps
  *              (entries of X are kept to 2^-32 of the largest it can have)
  *   out        laid out by its own strides; may be grad itself with the same strides
