@@ -659,7 +659,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_ns_product(const __grid_constan
     w.lane = lane;
     uint32_t lt = 0;
     bool ok = sound;
-    const bool broken = MODE == APPLY && a.user && *static_cast<volatile int32_t*>(a.status) != XRL_OK;      // an earlier launch
+    bool broken = false;                 // by an earlier launch (the whole warp with one answer)
+    if (MODE == APPLY && a.user) broken = __any_sync(0xFFFFFFFFu, *static_cast<volatile int32_t*>(a.status) != XRL_OK);
     for (int tile = first; ok && tile < total; tile += step) {
       const Tile t = tile_of<C::M, C::N, SYM>(a, tile);
       const int row = t.row + rank * kRows + q * 32, col = t.col + side * WC;

@@ -29,15 +29,22 @@ def test_a_word_that_is_set_while_a_call_runs_leaves_no_update(dtype, side, step
     side_stream, out = torch.cuda.Stream(), torch.empty_like(g)
     torch.cuda.synchronize()
     assert int(status) == 0 and bool(torch.isfinite(good).all())
-    for _ in range(6):                                            # (the stream stays full: the last call is far from done)
-        xrl.xrl_orthogonalise(g, steps=steps)
-    first = torch.cuda.Event()
-    first.record()
-    xrl.xrl_orthogonalise(g, steps=steps, out=out, device_status=status)
-    first.synchronize()                                           # the call's first launch is next: microseconds
-    time.sleep(5e-4)
-    with torch.cuda.stream(side_stream):
-        status.copy_(code, non_blocking=True)
-    torch.cuda.synchronize()
+    for _ in range(5):                                            # (again if the host was held up for the whole call)
+        for _ in range(6):
+            xrl.xrl_orthogonalise(g, steps=steps)
+        first, last = torch.cuda.Event(), torch.cuda.Event()
+        first.record()
+        xrl.xrl_orthogonalise(g, steps=steps, out=out, device_status=status)
+        last.record()
+        first.synchronize()                                       # the call's first launch is next: microseconds
+        time.sleep(5e-4)
+        with torch.cuda.stream(side_stream):
+            status.copy_(code, non_blocking=True)
+        side_stream.synchronize()
+        in_time = not last.query()
+        torch.cuda.synchronize()
+        if in_time:
+            break
+    assert in_time
     assert int(status) == 6 and bool(torch.isnan(out).all())
     assert torch.equal(xrl.xrl_orthogonalise(g, steps=steps, out=out, device_status=status), good) and int(status) == 0
